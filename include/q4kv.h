@@ -286,6 +286,41 @@ int q4kv_prefill_attention(const q4kv_spec* spec, const void* pool, int32_t n_bl
                            void* workspace, size_t workspace_bytes,
                            int32_t* status_flags, void* stream);
 
+/* ---- What comes before the cache: norm and rotation of the new rows ----
+ * The norm of every query and key head and the rotation by position in one pass, for models that have both or either
+ * (Section 3.6's families rotate; Gemma 3 also normalises each head).  Per head x[0 .. d_qk-1] of a row:
+ *   elements e < norm_dim, where a weight is given:  x_e * rsqrt(mean of their squares + eps) * (weight_e + weight_offset);
+ *   elements rot_begin .. rot_begin + rot_dim - 1 in pairs, pair j = 0 .. rot_dim/2 - 1 being elements (j, j + rot_dim/2) of
+ *   them, or (2j, 2j + 1) when interleaved:
+ *       (x_a, x_b) -> rot_scale * (x_a cos t - x_b sin t, x_b cos t + x_a sin t),   t = position * inv_freq[j].
+ * The angle is taken in 64 bits, everything else in binary32, rounded once to bfloat16 at the end.  A row's position is its
+ * cache position, as in q4kv_quantize_append: pos[a] + i for row new_offs[a] + i. */
+typedef struct {
+  int32_t norm_dim;          /* 0: no norm; else a multiple of 8, at most d_qk                                  */
+  int32_t rot_begin, rot_dim;/* rot_dim 0: no rotation; rot_begin a multiple of 8, rot_dim of 16 (interleaved: 8) */
+  int32_t interleaved;       /* 0: pairs lie rot_dim/2 apart, 1: pairs are neighbours                           */
+  float eps;                 /* above 0 where a norm is taken                                                   */
+  float weight_offset;       /* 0, or 1 where the model stores weight - 1                                       */
+  float rot_scale;           /* 1, or the attention factor of a stretched rotation                              */
+  int32_t reserved;          /* 0 */
+  const void* q_weight;      /* device, bf16 [norm_dim]; NULL: query heads are not normalised                   */
+  const void* k_weight;      /* the same for key heads                                                          */
+  const float* inv_freq;     /* device, float32 [rot_dim/2]                                                     */
+} q4kv_norm_rotation;
+
+/* Rows 0 .. total_new - 1 (rows before new_offs[0] or from new_offs[A] on belong to no agent and are left as they are).
+ *   pos      [A], new_offs [A+1]   device, as in q4kv_quantize_append; read, with inv_freq, before the preceding kernels of the
+ *                 stream have completed, like every length.  pos[a] < 0 raises Q4KV_FLAG_BAD_LENGTH and gives zeros.
+ *   q        bf16, row r at q + r * q_stride ELEMENTS, its n_q_heads heads of d_qk elements next to each other (a view of a
+ *            fused projection has q_stride > n_q_heads * d_qk); NULL with q_out NULL: no queries.  Strides: multiples of 8.
+ *   k        the same with n_kv_heads heads; NULL with k_out NULL: no keys
+ *   q_out    bf16 [total_new][n_q_heads][d_qk], k_out bf16 [total_new][n_kv_heads][d_qk]: what the append and attention calls
+ *            take.  q_out may be q itself (q_stride == n_q_heads * d_qk then), k_out k itself; any other overlap of an output
+ *            with an input or with the other output is refused. */
+int q4kv_norm_rope(const q4kv_spec* spec, const q4kv_norm_rotation* how, int32_t n_agents, const int32_t* pos,
+                   const int32_t* new_offs, int32_t total_new, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                   void* q_out, void* k_out, int32_t* status_flags, void* stream);
+
 /* Pack: gather one agent's blocks, all layers, through its block-table row into the persisted
  * layout (Appendix A, groups along head_dim): layer outermost, then logical block, then
  *   K_codes u32 [Hkv][256][d_qk/8] | K_scales f16 [Hkv][256][d_qk/64] | K_biases f16 [same] |
@@ -337,9 +372,21 @@ int q4kv_restore(const q4kv_spec* spec, const void* host_packed, size_t packed_b
                  int32_t n_blocks, const int32_t* block_table_row, void* dev_staging, size_t dev_staging_bytes,
                  int32_t* status_flags, void* copy_stream, void* unpack_stream);
 
+/* Copy blocks, layers layer_begin .. layer_begin + layer_count - 1, within a pool or from one pool to another of the same spec
+ * (the device half of q4kv_allocator_fork, _truncate and _compact; also for moving into a pool of another size).
+ *   copies   device int32 [n_copies][3]: source block in src_pool, destination block in dst_pool, tokens (0 .. 256)
+ * The 32-token chunks that hold the first `tokens` tokens of the block are copied whole, for every KV head; the rest of the
+ * destination is left as it was.  In one call no destination may be named twice, and within one pool no block may be both a
+ * source and a destination (which of the two contents a byte then gets is not defined); a block copied to itself stays as it is.
+ * src_pool == dst_pool requires src_blocks == dst_blocks.  A copy with a bad block id or token count raises its flag and is
+ * skipped. */
+int q4kv_copy_blocks(const q4kv_spec* spec, const void* src_pool, int32_t src_blocks, void* dst_pool, int32_t dst_blocks,
+                     int32_t layer_begin, int32_t layer_count, const int32_t* copies, int32_t n_copies, int32_t* status_flags,
+                     void* stream);
+
 /* ---- Block pool bookkeeping (Section 3.1 "Block Pool with Per-Agent Isolation") ----
- * Host-side policy only; no device memory is touched.  Every block belongs to at most one agent (isolation); agents
- * are kept in least-recently-used order.  When q4kv_allocator_reserve reports Q4KV_EWORKSPACE the pool is full: ask
+ * Host-side policy only; no device memory is touched.  Every block belongs to at most one agent (isolation) until the caller
+ * forks an agent, which shares whole blocks between parent and child; agents are kept in least-recently-used order.  When q4kv_allocator_reserve reports Q4KV_EWORKSPACE the pool is full: ask
  * q4kv_allocator_pick_victim for the least recently used agent that is not pinned, persist it (q4kv_save), release
  * it, and reserve again.  Not thread-safe: serialise the calls on one allocator. */
 typedef struct q4kv_allocator q4kv_allocator;
@@ -354,7 +401,27 @@ int q4kv_allocator_reserve(q4kv_allocator* allocator, int64_t agent_id, int32_t 
 int q4kv_allocator_touch(q4kv_allocator* allocator, int64_t agent_id);                    /* most recently used */
 int q4kv_allocator_pin(q4kv_allocator* allocator, int64_t agent_id, int32_t pinned);      /* pinned agents are never victims */
 int q4kv_allocator_pick_victim(const q4kv_allocator* allocator, int64_t* agent_id);       /* Q4KV_EWORKSPACE: none */
-int q4kv_allocator_release(q4kv_allocator* allocator, int64_t agent_id);                  /* its blocks become free */
+int q4kv_allocator_release(q4kv_allocator* allocator, int64_t agent_id);   /* its blocks become free (shared ones: with their last holder) */
+/* The agent's block-table row as q4kv_allocator_reserve writes it, without growing it or marking it used. */
+int q4kv_allocator_table(const q4kv_allocator* allocator, int64_t agent_id, int32_t* table_row, int32_t max_blocks);
+int32_t q4kv_allocator_block_holders(const q4kv_allocator* allocator, int32_t block);     /* agents that hold it; -1: no such block */
+/* Forks.  A new agent begins with the first n_tokens tokens of another (n_tokens at most the parent's length, which the caller
+ * keeps): it shares the parent's blocks that n_tokens fills, which neither writes again, and where n_tokens ends inside a block
+ * it gets a block of its own, to be filled by q4kv_copy_blocks before the child is used or the parent's block given up.
+ * copy (HOST, 3 entries) receives that copy (source, destination, tokens), or -1, -1, 0 when there is nothing to copy.  Parent
+ * and child are marked used.  EINVAL: unknown parent, known child, or n_tokens beyond the parent's blocks or the row;
+ * EWORKSPACE: no free block.  A negative return changes nothing; so with the next two. */
+int q4kv_allocator_fork(q4kv_allocator* allocator, int64_t parent_id, int64_t child_id, int32_t n_tokens, int32_t* table_row,
+                        int32_t max_blocks, int32_t* copy);
+/* Take an agent back to its first n_tokens tokens.  Blocks behind them are given up; where n_tokens ends inside a block that
+ * others share, the agent gets a block of its own in its place and copy names the copy, as above. */
+int q4kv_allocator_truncate(q4kv_allocator* allocator, int64_t agent_id, int32_t n_tokens, int32_t* table_row, int32_t max_blocks,
+                            int32_t* copy);
+/* Compact: up to max_copies times, the highest block in use moves to the lowest free one; the agents' lists follow at once, and
+ * copies (HOST, [max_copies][3]) receives the *n_copies moves for ONE q4kv_copy_blocks call (sources and destinations are
+ * disjoint), to be enqueued before anything that uses the new tables.  Read the tables again with q4kv_allocator_table.
+ * Fewer than max_copies moves: the blocks in use are now 0 .. (n_blocks - free) - 1. */
+int q4kv_allocator_compact(q4kv_allocator* allocator, int32_t* copies, int32_t max_copies, int32_t* n_copies);
 
 /* ---- Dense-batch shim (Section 3.4: BatchQuantizedKVCache.merge / extract) ----
  * The paper stacks caches of different lengths into one left-padded batch.  This library attends through block tables

@@ -29,7 +29,8 @@ EXPORTS = [
     "q4kv_container_header_bytes", "q4kv_container_write_header", "q4kv_container_read_header", "q4kv_save", "q4kv_restore",
     "q4kv_allocator_create", "q4kv_allocator_destroy", "q4kv_allocator_free_blocks", "q4kv_allocator_agent_blocks",
     "q4kv_allocator_reserve", "q4kv_allocator_touch", "q4kv_allocator_pin", "q4kv_allocator_pick_victim",
-    "q4kv_allocator_release", "q4kv_dense_bytes", "q4kv_merge_dense", "q4kv_extract_dense",
+    "q4kv_allocator_release", "q4kv_allocator_table", "q4kv_allocator_block_holders", "q4kv_allocator_fork",
+    "q4kv_allocator_truncate", "q4kv_allocator_compact", "q4kv_norm_rope", "q4kv_copy_blocks", "q4kv_dense_bytes", "q4kv_merge_dense", "q4kv_extract_dense",
 ]
 STATIC_SCRATCH_BYTES = 8 << 20
 WORKSPACE_HEADER_BYTES = 65536
@@ -56,8 +57,26 @@ class Batch(ctypes.Structure):
     _fields_ = [("n_agents", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("block_tables", ctypes.c_void_p)]
 
 
+class NormRotation(ctypes.Structure):
+    """q4kv_norm_rotation.  Keeps the tensors that it points to alive."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("norm_dim", "rot_begin", "rot_dim", "interleaved")] + \
+               [(n, ctypes.c_float) for n in ("eps", "weight_offset", "rot_scale")] + [("reserved", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "inv_freq")]
+
+    @classmethod
+    def make(cls, norm_dim=0, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0, rot_begin=0, rot_dim=0,
+             interleaved=False, inv_freq=None, rot_scale=1.0):
+        for w in (q_weight, k_weight):
+            assert w is None or (w.dtype == torch.bfloat16 and w.numel() == norm_dim)
+        assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.numel() == rot_dim // 2)
+        how = cls(norm_dim, rot_begin, rot_dim, int(bool(interleaved)), eps, weight_offset, rot_scale, 0, _ptr(q_weight),
+                  _ptr(k_weight), _ptr(inv_freq))
+        how.tensors = (q_weight, k_weight, inv_freq)
+        return how
+
+
 _lib = None
-_call = None                     # the four per-layer entry points through native marshalling (csrc/py_call.c)
+_call = None                     # the per-layer entry points through native marshalling (csrc/py_call.c)
 
 
 def lib() -> ctypes.CDLL:
@@ -125,6 +144,21 @@ def lib() -> ctypes.CDLL:
         L.q4kv_allocator_pick_victim.argtypes = [vp, ctypes.POINTER(i64)]
         L.q4kv_allocator_release.restype = ctypes.c_int
         L.q4kv_allocator_release.argtypes = [vp, i64]
+        i32p = ctypes.POINTER(i32)
+        L.q4kv_allocator_table.restype = ctypes.c_int
+        L.q4kv_allocator_table.argtypes = [vp, i64, i32p, i32]
+        L.q4kv_allocator_block_holders.restype = i32
+        L.q4kv_allocator_block_holders.argtypes = [vp, i32]
+        L.q4kv_allocator_fork.restype = ctypes.c_int
+        L.q4kv_allocator_fork.argtypes = [vp, i64, i64, i32, i32p, i32, i32p]
+        L.q4kv_allocator_truncate.restype = ctypes.c_int
+        L.q4kv_allocator_truncate.argtypes = [vp, i64, i32, i32p, i32, i32p]
+        L.q4kv_allocator_compact.restype = ctypes.c_int
+        L.q4kv_allocator_compact.argtypes = [vp, i32p, i32, i32p]
+        L.q4kv_norm_rope.restype = ctypes.c_int
+        L.q4kv_norm_rope.argtypes = [sp, ctypes.POINTER(NormRotation), i32, vp, vp, i32, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.q4kv_copy_blocks.restype = ctypes.c_int
+        L.q4kv_copy_blocks.argtypes = [sp, vp, i32, vp, i32, i32, i32, vp, i32, vp, vp]
         L.q4kv_dense_bytes.restype = sz
         L.q4kv_dense_bytes.argtypes = [sp, i32, i32]
         L.q4kv_merge_dense.restype = ctypes.c_int
@@ -137,7 +171,7 @@ def lib() -> ctypes.CDLL:
         L.q4kv_unpack.argtypes = [sp, vp, sz, i32, vp, i32, vp, vp, vp]
         from . import _call as call
         call.bind(*(ctypes.cast(getattr(L, "q4kv_" + n), ctypes.c_void_p).value for n in (
-            "quantize_append", "decode_attention", "append_decode_attention", "prefill_attention")))
+            "quantize_append", "decode_attention", "append_decode_attention", "prefill_attention", "norm_rope", "copy_blocks")))
         _lib, _call = L, call
     return _lib
 
@@ -171,6 +205,10 @@ def _stream():
     handle = torch.cuda.current_stream().cuda_stream
     _get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     return handle
+
+
+def _device():
+    return _get_device() if _get_device is not None else torch.cuda.current_device()
 
 
 def _check(code, where):
@@ -233,6 +271,20 @@ def q4kv_prefill_attention(spec, pool, n_blocks, layer, bt: Batch, kv_lens, q_of
                            window, q, softmax_scale, out, out_dtype, lse, workspace, status_flags=None):
     _check(_native().prefill(spec, pool, n_blocks, layer, bt, kv_lens, q_offs, total_q, max_q_len, max_kv_len, window, q,
                              softmax_scale, out, out_dtype, lse, workspace, status_flags, _stream()), "q4kv_prefill_attention")
+
+
+def q4kv_norm_rope(spec, how: NormRotation, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags=None):
+    """Norm and rotation of the new query and key rows.  q, k: bfloat16 [total_new][heads][d_qk] whose first stride is free (a
+    view of a fused projection); q_out, k_out contiguous, or the input itself."""
+    _check(_native().norm_rope(spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, _stream(),
+                               _device()), "q4kv_norm_rope")
+
+
+def q4kv_copy_blocks(spec, src_pool, src_blocks, dst_pool, dst_blocks, layer_begin, layer_count, copies, n_copies,
+                     status_flags=None):
+    """copies: int32 [n_copies][3] on the device, (source block, destination block, tokens)."""
+    _check(_native().copy_blocks(spec, src_pool, src_blocks, dst_pool, dst_blocks, layer_begin, layer_count, copies, n_copies,
+                                 status_flags, _stream(), _device()), "q4kv_copy_blocks")
 
 
 def q4kv_pack(spec, pool, n_blocks, block_table_row, n_tokens, dst, status_flags=None):
@@ -322,6 +374,32 @@ class Allocator:
         v = ctypes.c_int64(0)
         _check(lib().q4kv_allocator_pick_victim(self._h, ctypes.byref(v)), "q4kv_allocator_pick_victim")
         return v.value
+
+    def table(self, agent_id: int, max_blocks: int):
+        row = (ctypes.c_int32 * max_blocks)()
+        _check(lib().q4kv_allocator_table(self._h, agent_id, row, max_blocks), "q4kv_allocator_table")
+        return list(row)
+
+    def block_holders(self, block: int) -> int:
+        return lib().q4kv_allocator_block_holders(self._h, block)
+
+    def fork(self, parent_id: int, child_id: int, n_tokens: int, max_blocks: int):
+        """(the child's block-table row, the copy (source, destination, tokens) to make before it is used, or None)"""
+        row, copy = (ctypes.c_int32 * max_blocks)(), (ctypes.c_int32 * 3)()
+        _check(lib().q4kv_allocator_fork(self._h, parent_id, child_id, n_tokens, row, max_blocks, copy), "q4kv_allocator_fork")
+        return list(row), tuple(copy) if copy[2] else None
+
+    def truncate(self, agent_id: int, n_tokens: int, max_blocks: int):
+        """(the agent's block-table row, the copy to make before it is used, or None)"""
+        row, copy = (ctypes.c_int32 * max_blocks)(), (ctypes.c_int32 * 3)()
+        _check(lib().q4kv_allocator_truncate(self._h, agent_id, n_tokens, row, max_blocks, copy), "q4kv_allocator_truncate")
+        return list(row), tuple(copy) if copy[2] else None
+
+    def compact(self, max_copies: int):
+        """The moves (source, destination, 256) to be made by one q4kv_copy_blocks call."""
+        copies, n = (ctypes.c_int32 * (3 * max(1, max_copies)))(), ctypes.c_int32(0)
+        _check(lib().q4kv_allocator_compact(self._h, copies, max_copies, ctypes.byref(n)), "q4kv_allocator_compact")
+        return [tuple(copies[3 * i:3 * i + 3]) for i in range(n.value)]
 
     def release(self, agent_id: int):
         _check(lib().q4kv_allocator_release(self._h, agent_id), "q4kv_allocator_release")

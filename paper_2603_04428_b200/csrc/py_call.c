@@ -2,6 +2,7 @@
  * C call.  Bound by interpreter overhead: through ctypes the smallest decode call spent 7.3 us on the host, 1.6 of them on the
  * conversion of its nineteen arguments and 1.4 on the pointers of its nine tensors; the launch itself takes 2.9.  Here 5.1 us,
  * below what the GPU takes (6.5); an append 5.5 -> 4.0.  The other entry points are called rarely and stay with ctypes.
+ * The later calls (norm and rotation, shared prefixes, block copies) also refuse tensors of another device than the current one.
  * The entry points' addresses come from the ctypes library (bind), so there is one copy of the library in the process. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -19,7 +20,11 @@ static int (*f_append_decode)(const q4kv_spec*, void*, int32_t, int32_t, const q
 static int (*f_prefill)(const q4kv_spec*, const void*, int32_t, int32_t, const q4kv_batch*, const int32_t*, const int32_t*,
                         int32_t, int32_t, int32_t, int32_t, const void*, float, void*, int32_t, float*, void*, size_t, int32_t*,
                         void*);
-static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes;
+static int (*f_norm_rope)(const q4kv_spec*, const q4kv_norm_rotation*, int32_t, const int32_t*, const int32_t*, int32_t, const void*,
+                          int64_t, const void*, int64_t, void*, void*, int32_t*, void*);
+static int (*f_copy_blocks)(const q4kv_spec*, const void*, int32_t, void*, int32_t, int32_t, int32_t, const int32_t*, int32_t,
+                            int32_t*, void*);
+static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes, *s_get_device, *s_stride, *s_element_size;
 
 /* A device pointer: None, an integer, or a contiguous CUDA tensor. */
 static int get_ptr(PyObject* o, void** out) {
@@ -146,18 +151,97 @@ static PyObject* prefill(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
-/* bind(append, decode, append_decode, prefill): the entry points' addresses */
+/* The same as get_ptr for a tensor that has to lie on device dev (an integer or None is taken as it is). */
+static int on_device(PyObject* o, long dev) {
+  if (o == Py_None || PyLong_Check(o)) return 1;
+  PyObject* r = PyObject_CallMethodNoArgs(o, s_get_device);
+  if (!r) return 0;
+  const long at = PyLong_AsLong(r);
+  Py_DECREF(r);
+  if (at == -1 && PyErr_Occurred()) return 0;
+  if (at != dev) { PyErr_SetString(PyExc_AssertionError, "a tensor lies on another device than the current one"); return 0; }
+  return 1;
+}
+static int get_ptr_on(PyObject* o, long dev, void** out) { return get_ptr(o, out) && on_device(o, dev); }
+/* Rows [tokens][heads][d] of 16-bit elements whose first stride is free: pointer and stride. */
+static int get_rows(PyObject* o, long dev, void** out, int64_t heads, int64_t d, int64_t rows, int64_t* stride) {
+  int64_t st[3];
+  PyObject* r;
+  *stride = heads * d;
+  if (o == Py_None) { *out = NULL; return 1; }
+  if (!(r = PyObject_GetAttr(o, s_is_cuda))) return 0;
+  int ok = PyObject_IsTrue(r);
+  Py_DECREF(r);
+  if (ok < 0) return 0;
+  if (!ok) { PyErr_SetString(PyExc_AssertionError, "rows come from CUDA tensors"); return 0; }
+  if (!on_device(o, dev) || !(r = PyObject_CallMethodNoArgs(o, s_stride))) return 0;
+  ok = PyArg_ParseTuple(r, "LLL", &st[0], &st[1], &st[2]);
+  Py_DECREF(r);
+  if (!ok) return 0;
+  if (!(r = PyObject_CallMethodNoArgs(o, s_element_size))) return 0;
+  ok = PyLong_AsLong(r) == 2;
+  Py_DECREF(r);
+  if (PyErr_Occurred()) return 0;
+  const Py_ssize_t n = PyObject_Length(o);
+  if (n < 0) return 0;
+  if (!ok || (n > 0 && rows > 0 && (n < rows || (st[2] != 1 && d > 1) || (st[1] != d && heads > 1)))) {
+    PyErr_SetString(PyExc_AssertionError, "rows are bfloat16 [tokens][heads][d] with whole heads next to each other");
+    return 0;
+  }
+  if (rows > 1) *stride = st[0];
+  if (!(r = PyObject_CallMethodNoArgs(o, s_data_ptr))) return 0;
+  *out = PyLong_AsVoidPtr(r);
+  Py_DECREF(r);
+  return !(*out == NULL && PyErr_Occurred());
+}
+/* spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, stream, device */
+static PyObject* norm_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  q4kv_spec spec;
+  q4kv_norm_rotation how;
+  void *pos, *offs, *q, *k, *qo, *ko, *flags, *stream;
+  int32_t agents, total, dev;
+  int64_t qs, ks;
+  int rc;
+  if (!count(n, 13) || !get_struct(a[0], &spec, sizeof spec) || !get_struct(a[1], &how, sizeof how) || !get_i32(a[2], &agents) ||
+      !get_i32(a[12], &dev) || !get_ptr_on(a[3], dev, &pos) || !get_ptr_on(a[4], dev, &offs) || !get_i32(a[5], &total) ||
+      !get_rows(a[6], dev, &q, spec.n_q_heads, spec.d_qk, total, &qs) ||
+      !get_rows(a[7], dev, &k, spec.n_kv_heads, spec.d_qk, total, &ks) || !get_ptr_on(a[8], dev, &qo) ||
+      !get_ptr_on(a[9], dev, &ko) || !get_ptr_on(a[10], dev, &flags) || !get_ptr(a[11], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_norm_rope(&spec, &how, agents, pos, offs, total, q, qs, k, ks, qo, ko, flags, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+/* spec, src_pool, src_blocks, dst_pool, dst_blocks, layer_begin, layer_count, copies, n_copies, status_flags, stream, device */
+static PyObject* copy_blocks(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  q4kv_spec spec;
+  void *src, *dst, *copies, *flags, *stream;
+  int32_t ns, nd, l0, nl, nc, dev;
+  int rc;
+  if (!count(n, 12) || !get_struct(a[0], &spec, sizeof spec) || !get_i32(a[11], &dev) || !get_ptr_on(a[1], dev, &src) ||
+      !get_i32(a[2], &ns) || !get_ptr_on(a[3], dev, &dst) || !get_i32(a[4], &nd) || !get_i32(a[5], &l0) || !get_i32(a[6], &nl) ||
+      !get_ptr_on(a[7], dev, &copies) || !get_i32(a[8], &nc) || !get_ptr_on(a[9], dev, &flags) || !get_ptr(a[10], &stream))
+    return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_copy_blocks(&spec, src, ns, dst, nd, l0, nl, copies, nc, flags, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+/* bind(append, decode, append_decode, prefill, norm_rope, copy_blocks): the entry points' addresses */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[4];
-  if (!count(n, 4)) return NULL;
-  for (int i = 0; i < 4; ++i)
+  void* p[6];
+  if (!count(n, 6)) return NULL;
+  for (int i = 0; i < 6; ++i)
     if (!get_ptr(a[i], &p[i])) return NULL;
   *(void**)&f_append = p[0]; *(void**)&f_decode = p[1]; *(void**)&f_append_decode = p[2]; *(void**)&f_prefill = p[3];
+  *(void**)&f_norm_rope = p[4]; *(void**)&f_copy_blocks = p[5];
   Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {FAST(append), FAST(decode), FAST(append_decode), FAST(prefill), FAST(bind), {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {FAST(append), FAST(decode), FAST(append_decode), FAST(prefill), FAST(norm_rope),
+                                FAST(copy_blocks), FAST(bind), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__call(void) {
@@ -165,5 +249,8 @@ PyMODINIT_FUNC PyInit__call(void) {
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_nbytes = PyUnicode_InternFromString("nbytes");
+  s_get_device = PyUnicode_InternFromString("get_device");
+  s_stride = PyUnicode_InternFromString("stride");
+  s_element_size = PyUnicode_InternFromString("element_size");
   return PyModule_Create(&module);
 }

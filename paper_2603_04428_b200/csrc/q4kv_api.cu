@@ -1,8 +1,11 @@
 // C ABI of libq4kv.so: host-side validation, sizing and dispatch.  See include/q4kv.h for
 // the contract of every entry point.
+#include <cmath>
+
 #include "q4kv_layout.cuh"
 
 using namespace q4kv;
+using std::isfinite;
 
 namespace {
 
@@ -306,6 +309,64 @@ int q4kv_prefill_attention(const q4kv_spec* spec, const void* pool, int32_t n_bl
     e = launch_attention_generic(y, pool, n_blocks, layer, *batch, kv_lens, q_offs, total_q, max_q_len, max_kv_len,
                                  window, q, softmax_scale, out, out_dtype, lse, workspace, status_flags,
                                  (cudaStream_t)stream);
+  return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
+}
+
+int q4kv_norm_rope(const q4kv_spec* spec, const q4kv_norm_rotation* how, int32_t n_agents, const int32_t* pos,
+                   const int32_t* new_offs, int32_t total_new, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                   void* q_out, void* k_out, int32_t* status_flags, void* stream) {
+  const int rc = check_spec(spec);
+  if (rc) return rc;
+  if (!how || n_agents < 0 || total_new < 0 || how->reserved != 0) return Q4KV_EINVAL;
+  const int d = spec->d_qk;
+  if (how->norm_dim < 0 || how->norm_dim > d || how->rot_dim < 0 || how->rot_dim > d || how->rot_begin < 0 ||
+      how->rot_begin > d - how->rot_dim || (how->interleaved != 0 && how->interleaved != 1))
+    return Q4KV_EINVAL;
+  if (how->norm_dim == 0 ? how->q_weight || how->k_weight : !(how->eps > 0.f) || !isfinite(how->eps) || !isfinite(how->weight_offset))
+    return Q4KV_EINVAL;
+  if (how->rot_dim > 0 && (!how->inv_freq || !isfinite(how->rot_scale))) return Q4KV_EINVAL;
+  if (how->norm_dim % 8 || how->rot_begin % 8 || how->rot_dim % (how->interleaved ? 8 : 16)) return Q4KV_EUNSUPPORTED;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return Q4KV_EINVAL;
+  if (total_new == 0 || n_agents == 0 || (!q && !k)) return Q4KV_OK;
+  if (!pos || !new_offs) return Q4KV_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(how->q_weight) ||
+      !aligned16(how->k_weight))
+    return Q4KV_EINVAL;
+  const int64_t q_row = (int64_t)spec->n_q_heads * d, k_row = (int64_t)spec->n_kv_heads * d;
+  constexpr int64_t kMost = INT64_MAX / 4 / INT32_MAX;     // byte offsets of every row stay within 63 bits
+  if ((q && (q_stride < q_row || q_stride % 8 || q_stride > kMost)) || (k && (k_stride < k_row || k_stride % 8 || k_stride > kMost)))
+    return Q4KV_EINVAL;
+  struct Range { uintptr_t lo, hi; };
+  auto range = [&](const void* p, int64_t row, int64_t stride) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    return p ? Range{lo, lo + 2 * (uintptr_t)((total_new - 1) * stride + row)} : Range{0, 0};
+  };
+  auto meet = [](Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; };
+  const Range qi = range(q, q_row, q_stride), ki = range(k, k_row, k_stride), qo = range(q_out, q_row, q_row),
+              ko = range(k_out, k_row, k_row);
+  const bool q_same = q_out == q && q_stride == q_row, k_same = k_out == k && k_stride == k_row;
+  if (meet(qo, ko) || meet(qo, ki) || meet(ko, qi) || (!q_same && meet(qo, qi)) || (!k_same && meet(ko, ki))) return Q4KV_EINVAL;
+  const Layout y = make_layout(*spec, 1);
+  const cudaError_t e = launch_norm_rope(y, *how, n_agents, pos, new_offs, total_new, q, q_stride, k, k_stride, q_out, k_out,
+                                         status_flags, (cudaStream_t)stream);
+  return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
+}
+
+int q4kv_copy_blocks(const q4kv_spec* spec, const void* src_pool, int32_t src_blocks, void* dst_pool, int32_t dst_blocks,
+                     int32_t layer_begin, int32_t layer_count, const int32_t* copies, int32_t n_copies, int32_t* status_flags,
+                     void* stream) {
+  const int rc = check_spec(spec);
+  if (rc) return rc;
+  if (!src_pool || !dst_pool || src_blocks <= 0 || dst_blocks <= 0 || layer_begin < 0 || layer_count < 0 ||
+      layer_begin > spec->n_layers - layer_count || n_copies < 0 || (src_pool == dst_pool && src_blocks != dst_blocks))
+    return Q4KV_EINVAL;
+  if (!aligned16(src_pool) || !aligned16(dst_pool)) return Q4KV_EINVAL;
+  if (n_copies == 0 || layer_count == 0) return Q4KV_OK;
+  if (!copies) return Q4KV_EINVAL;
+  if ((int64_t)n_copies * spec->n_kv_heads > INT32_MAX || layer_count > 65535) return Q4KV_EUNSUPPORTED;    // grid limits
+  const Layout y = make_layout(*spec, src_blocks);
+  const cudaError_t e = launch_copy_blocks(y, src_pool, src_blocks, dst_pool, dst_blocks, layer_begin, layer_count, copies, n_copies,
+                                           status_flags, (cudaStream_t)stream);
   return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
 }
 

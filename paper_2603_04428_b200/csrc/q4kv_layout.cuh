@@ -127,6 +127,11 @@ cudaError_t launch_unpack_layers(const Layout& y, const void* src, int n_tokens,
                                  const int32_t* row, int32_t* flags, cudaStream_t st, int layer0, int layer_count);
 cudaError_t launch_dense_exchange(const Layout& y, void* pool, int n_blocks, int layer, const q4kv_batch& b,
                                   const int32_t* kv_lens, int T, void* dense, bool to_pool, int32_t* flags, cudaStream_t st);
+cudaError_t launch_copy_blocks(const Layout& y, const void* src, int src_blocks, void* dst, int dst_blocks, int layer0, int layers,
+                               const int32_t* copies, int n_copies, int32_t* flags, cudaStream_t st);
+cudaError_t launch_norm_rope(const Layout& y, const q4kv_norm_rotation& how, int n_agents, const int32_t* pos, const int32_t* offs,
+                             int rows, const void* q, long long q_stride, const void* k, long long k_stride, void* q_out, void* k_out,
+                             int32_t* flags, cudaStream_t st);
 cudaError_t launch_attention_generic(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b,
                                      const int32_t* kv_lens, const int32_t* q_offs, int total_q, int max_q_len,
                                      int max_kv_len, int window, const void* q, float scale, void* out,
