@@ -30,7 +30,8 @@ EXPORTS = [
     "q4kv_allocator_create", "q4kv_allocator_destroy", "q4kv_allocator_free_blocks", "q4kv_allocator_agent_blocks",
     "q4kv_allocator_reserve", "q4kv_allocator_touch", "q4kv_allocator_pin", "q4kv_allocator_pick_victim",
     "q4kv_allocator_release", "q4kv_allocator_table", "q4kv_allocator_block_holders", "q4kv_allocator_fork",
-    "q4kv_allocator_truncate", "q4kv_allocator_compact", "q4kv_norm_rope", "q4kv_copy_blocks", "q4kv_dense_bytes", "q4kv_merge_dense", "q4kv_extract_dense",
+    "q4kv_allocator_truncate", "q4kv_allocator_compact", "q4kv_norm_rope", "q4kv_copy_blocks",
+    "q4kv_workspace_bytes_shared_prefix", "q4kv_shared_prefix_decode_attention", "q4kv_dense_bytes", "q4kv_merge_dense", "q4kv_extract_dense",
 ]
 STATIC_SCRATCH_BYTES = 8 << 20
 WORKSPACE_HEADER_BYTES = 65536
@@ -157,6 +158,11 @@ def lib() -> ctypes.CDLL:
         L.q4kv_allocator_compact.argtypes = [vp, i32p, i32, i32p]
         L.q4kv_norm_rope.restype = ctypes.c_int
         L.q4kv_norm_rope.argtypes = [sp, ctypes.POINTER(NormRotation), i32, vp, vp, i32, vp, i64, vp, i64, vp, vp, vp, vp]
+        L.q4kv_workspace_bytes_shared_prefix.restype = sz
+        L.q4kv_workspace_bytes_shared_prefix.argtypes = [sp, i32, i32, i32]
+        L.q4kv_shared_prefix_decode_attention.restype = ctypes.c_int
+        L.q4kv_shared_prefix_decode_attention.argtypes = [sp, vp, i32, i32, bp, vp, i32, vp, vp, i32, vp, f32, vp, i32, vp, vp, sz,
+                                                          vp, vp]
         L.q4kv_copy_blocks.restype = ctypes.c_int
         L.q4kv_copy_blocks.argtypes = [sp, vp, i32, vp, i32, i32, i32, vp, i32, vp, vp]
         L.q4kv_dense_bytes.restype = sz
@@ -171,7 +177,8 @@ def lib() -> ctypes.CDLL:
         L.q4kv_unpack.argtypes = [sp, vp, sz, i32, vp, i32, vp, vp, vp]
         from . import _call as call
         call.bind(*(ctypes.cast(getattr(L, "q4kv_" + n), ctypes.c_void_p).value for n in (
-            "quantize_append", "decode_attention", "append_decode_attention", "prefill_attention", "norm_rope", "copy_blocks")))
+            "quantize_append", "decode_attention", "append_decode_attention", "prefill_attention", "norm_rope", "copy_blocks",
+            "shared_prefix_decode_attention")))
         _lib, _call = L, call
     return _lib
 
@@ -271,6 +278,18 @@ def q4kv_prefill_attention(spec, pool, n_blocks, layer, bt: Batch, kv_lens, q_of
                            window, q, softmax_scale, out, out_dtype, lse, workspace, status_flags=None):
     _check(_native().prefill(spec, pool, n_blocks, layer, bt, kv_lens, q_offs, total_q, max_q_len, max_kv_len, window, q,
                              softmax_scale, out, out_dtype, lse, workspace, status_flags, _stream()), "q4kv_prefill_attention")
+
+
+def q4kv_workspace_bytes_shared_prefix(spec: Spec, n_agents: int, max_kv_len: int, n_groups: int) -> int:
+    return lib().q4kv_workspace_bytes_shared_prefix(ctypes.byref(spec), n_agents, max_kv_len, n_groups)
+
+
+def q4kv_shared_prefix_decode_attention(spec, pool, n_blocks, layer, bt: Batch, kv_lens, max_kv_len, group_offs, prefix_lens,
+                                        n_groups, q, softmax_scale, out, out_dtype, lse, workspace, status_flags=None):
+    """Decode attention for agents whose groups share prefixes: a prefix's keys and values are read once for its group."""
+    _check(_native().shared_prefix(spec, pool, n_blocks, layer, bt, kv_lens, max_kv_len, group_offs, prefix_lens, n_groups, q,
+                                   softmax_scale, out, out_dtype, lse, workspace, status_flags, _stream(), _device()),
+           "q4kv_shared_prefix_decode_attention")
 
 
 def q4kv_norm_rope(spec, how: NormRotation, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags=None):

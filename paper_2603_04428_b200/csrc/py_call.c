@@ -24,6 +24,8 @@ static int (*f_norm_rope)(const q4kv_spec*, const q4kv_norm_rotation*, int32_t, 
                           int64_t, const void*, int64_t, void*, void*, int32_t*, void*);
 static int (*f_copy_blocks)(const q4kv_spec*, const void*, int32_t, void*, int32_t, int32_t, int32_t, const int32_t*, int32_t,
                             int32_t*, void*);
+static int (*f_shared_prefix)(const q4kv_spec*, const void*, int32_t, int32_t, const q4kv_batch*, const int32_t*, int32_t, const int32_t*,
+                              const int32_t*, int32_t, const void*, float, void*, int32_t, float*, void*, size_t, int32_t*, void*);
 static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes, *s_get_device, *s_stride, *s_element_size;
 
 /* A device pointer: None, an integer, or a contiguous CUDA tensor. */
@@ -228,20 +230,39 @@ static PyObject* copy_blocks(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
-/* bind(append, decode, append_decode, prefill, norm_rope, copy_blocks): the entry points' addresses */
+/* spec, pool, n_blocks, layer, batch, kv_lens, max_kv_len, group_offs, prefix_lens, n_groups, q .. stream, device */
+static PyObject* shared_prefix(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  Head h;
+  Tail t;
+  void *lens, *offs, *prefix;
+  int32_t max_kv, groups, dev;
+  int rc;
+  if (!count(n, 19) || !get_head(a, &h) || !get_i32(a[18], &dev) || !on_device(a[1], dev) || !get_ptr_on(a[5], dev, &lens) ||
+      !get_i32(a[6], &max_kv) || !get_ptr_on(a[7], dev, &offs) || !get_ptr_on(a[8], dev, &prefix) || !get_i32(a[9], &groups) ||
+      !get_tail(a + 10, &t))
+    return NULL;
+  for (int i = 10; i < 17; ++i)                            /* q, out, lse, workspace, status_flags (numbers pass) */
+    if (i != 11 && i != 13 && !on_device(a[i], dev)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  rc = f_shared_prefix(&h.spec, h.pool, h.n_blocks, h.layer, &h.batch, lens, max_kv, offs, prefix, groups, t.q, t.scale, t.out,
+                       t.out_dtype, t.lse, t.ws, t.ws_bytes, t.flags, t.stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+/* bind(append, decode, append_decode, prefill, norm_rope, copy_blocks, shared_prefix): the entry points' addresses */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-  void* p[6];
-  if (!count(n, 6)) return NULL;
-  for (int i = 0; i < 6; ++i)
+  void* p[7];
+  if (!count(n, 7)) return NULL;
+  for (int i = 0; i < 7; ++i)
     if (!get_ptr(a[i], &p[i])) return NULL;
   *(void**)&f_append = p[0]; *(void**)&f_decode = p[1]; *(void**)&f_append_decode = p[2]; *(void**)&f_prefill = p[3];
-  *(void**)&f_norm_rope = p[4]; *(void**)&f_copy_blocks = p[5];
+  *(void**)&f_norm_rope = p[4]; *(void**)&f_copy_blocks = p[5]; *(void**)&f_shared_prefix = p[6];
   Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(append), FAST(decode), FAST(append_decode), FAST(prefill), FAST(norm_rope),
-                                FAST(copy_blocks), FAST(bind), {NULL, NULL, 0, NULL}};
+                                FAST(copy_blocks), FAST(shared_prefix), FAST(bind), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__call(void) {

@@ -251,6 +251,40 @@ int q4kv_decode_attention_layers(const q4kv_spec* spec, void* pool, int32_t n_bl
   return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
 }
 
+size_t q4kv_workspace_bytes_shared_prefix(const q4kv_spec* spec, int32_t n_agents, int32_t max_kv_len, int32_t n_groups) {
+  if (check_spec(spec) != Q4KV_OK || n_agents < 0 || max_kv_len < 0 || n_groups < 0) return 0;
+  const Layout y = make_layout(*spec, 1);
+  const int agents = n_agents > 0 ? n_agents : 1;
+  if (!shared_prefix_supported(y, agents, max_kv_len) || n_groups > agents) return 0;
+  return kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, agents, n_groups > 0 ? n_groups : 1);
+}
+
+int q4kv_shared_prefix_decode_attention(const q4kv_spec* spec, const void* pool, int32_t n_blocks, int32_t layer,
+                                        const q4kv_batch* batch, const int32_t* kv_lens, int32_t max_kv_len,
+                                        const int32_t* group_offs, const int32_t* prefix_lens, int32_t n_groups,
+                                        const void* q, float softmax_scale, void* out, int32_t out_dtype, float* lse,
+                                        void* workspace, size_t workspace_bytes, int32_t* status_flags, void* stream) {
+  int rc = check_spec(spec);
+  if (rc) return rc;
+  if ((rc = check_batch(batch))) return rc;
+  if (!pool || n_blocks <= 0 || layer < 0 || layer >= spec->n_layers || max_kv_len < 0 || n_groups < 0) return Q4KV_EINVAL;
+  if (out_dtype != Q4KV_OUT_F32 && out_dtype != Q4KV_OUT_BF16) return Q4KV_EINVAL;
+  if (batch->n_agents == 0) return Q4KV_OK;
+  if (!kv_lens || !group_offs || !prefix_lens || !q || !out || !workspace || n_groups == 0 || n_groups > batch->n_agents)
+    return Q4KV_EINVAL;
+  if (!aligned16(pool) || !aligned16(q) || !aligned16(out) || !aligned16(workspace)) return Q4KV_EINVAL;
+  if (batch->max_blocks > INT32_MAX / kBlockTokens) return Q4KV_EUNSUPPORTED;
+  const int cap = batch->max_blocks * kBlockTokens;
+  if (max_kv_len == 0 || max_kv_len > cap) max_kv_len = cap;
+  const Layout y = make_layout(*spec, n_blocks);
+  if (!shared_prefix_supported(y, batch->n_agents, max_kv_len) || !tiles_allowed(spec, softmax_scale)) return Q4KV_EUNSUPPORTED;
+  if (workspace_bytes < kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, batch->n_agents, n_groups)) return Q4KV_EWORKSPACE;
+  const cudaError_t e = launch_shared_prefix(y, pool, n_blocks, layer, *batch, kv_lens, max_kv_len, group_offs, prefix_lens, n_groups, q,
+                                             softmax_scale, out, out_dtype, lse, (uint8_t*)workspace + kWorkspaceHeaderBytes,
+                                             status_flags, (cudaStream_t)stream);
+  return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
+}
+
 int q4kv_prefill_attention(const q4kv_spec* spec, const void* pool, int32_t n_blocks, int32_t layer,
                            const q4kv_batch* batch, const int32_t* kv_lens, const int32_t* q_offs,
                            int32_t total_q, int32_t max_q_len, int32_t max_kv_len,

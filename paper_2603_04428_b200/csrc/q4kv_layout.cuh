@@ -200,6 +200,13 @@ cudaError_t launch_merge_prefill(const Layout& y, int total_q, int n_splits, con
                                  // q_offs: the rows of agents with one query are left as they are
                                  const int32_t* q_offs = nullptr, int n_agents = 0);
 
+// Decode of agents that share prefixes (d_qk = d_v in {128, 256}, d_qk 192 / d_v 128)
+bool shared_prefix_supported(const Layout& y, int n_agents, int max_kv_len);
+size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups);
+cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
+                                 int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
+                                 float scale, void* out, int out_dtype, float* lse, void* ws, int32_t* flags, cudaStream_t st);
+
 // Decode on the MLA-latent cache (d_qk 576, d_v 512 aliasing K, one KV head, at most 16 query heads): a key-split
 // attention kernel -- on a binary16 tile of the dequantized keys, or, with on_codes, on the 4-bit codes themselves
 // (exact products) -- followed by the combination of the records.

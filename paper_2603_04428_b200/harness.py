@@ -78,6 +78,20 @@ class DeviceCache:
                                 float(scale), out, out_dtype, lse, ws, self.flags)
         return out, lse
 
+    def shared_prefix_decode(self, layer, kv_lens, group_offs, prefix_lens, q_bits, scale, out_dtype=B.OUT_F32, want_lse=True,
+                             max_kv_len=0):
+        q = bf16_dev(q_bits) if isinstance(q_bits, np.ndarray) else q_bits
+        A, G = q.shape[0], len(prefix_lens)
+        lens_d, offs_d, pre_d = (x if torch.is_tensor(x) else dev(np.asarray(x, dtype=np.int32)) for x in (kv_lens, group_offs, prefix_lens))
+        out = torch.empty((A, self.spec.n_q_heads, self.spec.d_v), device="cuda",
+                          dtype=torch.float32 if out_dtype == B.OUT_F32 else torch.bfloat16)
+        lse = torch.empty((A, self.spec.n_q_heads), dtype=torch.float32, device="cuda") if want_lse else None
+        ws = torch.empty(B.q4kv_workspace_bytes_shared_prefix(self.spec, A, max_kv_len or self.bt.max_blocks * 256, G),
+                         dtype=torch.uint8, device="cuda")
+        B.q4kv_shared_prefix_decode_attention(self.spec, self.pool, self.n_blocks, layer, self.bt, lens_d, max_kv_len, offs_d, pre_d,
+                                              G, q, float(scale), out, out_dtype, lse, ws, self.flags)
+        return out, lse
+
     def append_decode(self, layer, kv_lens, window, k_bits, v_bits, q_bits, scale, out_dtype=B.OUT_F32, bt=None):
         """One new token per agent appended at position kv_len - 1 and attended, in one launch."""
         q = bf16_dev(q_bits) if isinstance(q_bits, np.ndarray) else q_bits

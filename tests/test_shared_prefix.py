@@ -1,0 +1,395 @@
+"""Attention of agents that share prefixes, against the float64 oracle's decode attention of each agent alone."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import q4kv_oracle as O
+from paper_2603_04428_b200 import binding as B, synth
+
+ATOL, RTOL_ROW = 2e-3, 1e-2      # the library's parity bounds for unit-variance caches (binary32 output)
+
+
+class Forked:
+    """Groups [(prefix, [own tokens or None for an idle agent])] as an oracle pool and a device pool.  On the device, what the call
+    must not read is poison: table entries of whole prefix blocks and the prefix's tokens in the copied block (agents but the first with
+    tokens), and every slot past a length."""
+
+    def __init__(self, shape, groups, seed, sb_dtype=0, layers=1, edit=None):
+        from paper_2603_04428_b200 import harness as H
+        hq, hkv, d, dv = shape
+        self.shape, self.groups = shape, groups
+        rows, lens, n, lead_of = [], [], 0, []
+        g = synth.rng(seed, 1)
+        poison, copies = [], []
+        for prefix, tails in groups:
+            whole, part = divmod(prefix, 256)
+            shared = list(range(n, n + whole))
+            n += whole
+            lead = None
+            for t in tails:
+                if t is None:
+                    rows.append(([], []))
+                    lens.append(0)
+                    continue
+                mine = list(range(n, n + -(-(prefix + t) // 256) - whole))
+                n += len(mine)
+                first = lead is None
+                if part and not first:
+                    copies.append((lead[whole], mine[0], part))
+                    poison.append((mine[0], 0, part))
+                elif first:
+                    lead = shared + mine
+                if (prefix + t) % 256:
+                    poison.append(((shared + mine)[-1], (prefix + t) % 256, 256))
+                rows.append((shared + mine, (shared if first else [-1] * whole) + mine))
+                lens.append(prefix + t)
+        self.n_blocks = n + 2
+        order = g.permutation(self.n_blocks)
+        wide = max(1, max(len(r[0]) for r in rows))
+        real = np.full((len(rows), wide), -1, np.int32)
+        told = real.copy()
+        for i, (a, b) in enumerate(rows):
+            real[i, :len(a)] = [order[x] for x in a]
+            told[i, :len(b)] = [order[x] if x >= 0 else -1 for x in b]
+        self.lens, self.tables = lens, real
+        self.offs = np.concatenate([[0], np.cumsum([len(t) for _, t in groups])]).astype(np.int32)
+        self.prefix = [p for p, _ in groups]
+        self.opool = O.Pool(O.Spec(layers, hq, hkv, d, dv, sb_dtype=sb_dtype), self.n_blocks)
+        for name, dd in (("K", d), ("V", dv)):
+            x = synth.bf16_bits_to_f32(synth.normal_bf16(seed, 2 if name == "K" else 3, (layers, self.n_blocks, hkv, 256, dd)))
+            codes, sc, bi = O.quantize_rows(x, sb_dtype)
+            getattr(self.opool, name + "c")[:] = O.pack_codes(codes)
+            getattr(self.opool, name + "s")[:] = sc
+            getattr(self.opool, name + "b")[:] = bi
+        if edit:
+            edit(self)
+        for a, b, m in copies:
+            for t in self.opool.tensors():
+                t[:, order[b], :, :m] = t[:, order[a], :, :m]
+        clean = [t.copy() for t in self.opool.tensors()]
+        nan = np.float16(np.nan) if sb_dtype == 0 else np.uint16(0x7FC0)
+        for b, lo, hi in poison:
+            for name in ("Kc", "Vc"):
+                getattr(self.opool, name)[:, order[b], :, lo:hi] = 0xFFFFFFFF
+            for name in ("Ks", "Kb", "Vs", "Vb"):
+                getattr(self.opool, name)[:, order[b], :, lo:hi] = nan
+        image = O.pack(self.opool, np.arange(self.n_blocks), self.n_blocks * 256)
+        for t, c in zip(self.opool.tensors(), clean):
+            t[:] = c
+        self.dc = H.DeviceCache(layers, hq, hkv, d, dv, False, self.n_blocks, told, sb_dtype=sb_dtype)
+        B.q4kv_unpack(self.dc.spec, H.dev(image), self.n_blocks * 256, self.dc.pool, self.n_blocks,
+                      H.dev(np.arange(self.n_blocks, dtype=np.int32)), self.dc.flags)
+
+    def q(self, stream=7):
+        return synth.normal_bf16(5, stream, (len(self.lens), self.shape[0], self.shape[2]))
+
+    def want(self, q, scale, layer=0):
+        return O.decode_attention(self.opool, layer, self.tables, self.lens, 0, synth.bf16_bits_to_f32(q), scale)
+
+    def run(self, q, scale, **kw):
+        return self.dc.shared_prefix_decode(kw.pop("layer", 0), self.lens, self.offs, self.prefix, q, scale, **kw)
+
+
+def close(out, lse, want, want_lse, bf16=False):
+    out = out.double().cpu().numpy()
+    assert np.all(np.isfinite(out))
+    err, extra = np.abs(out - want), 2.0 ** -8 * np.abs(want) if bf16 else 0.0
+    assert (err - extra).max() <= ATOL, err.max()
+    row = (err - extra).reshape(-1, want.shape[-1]).max(1)
+    assert np.all(row <= RTOL_ROW * np.abs(want).reshape(-1, want.shape[-1]).max(1) + 1e-30)
+    if lse is not None:
+        lse = lse.double().cpu().numpy()
+        assert np.array_equal(np.isneginf(lse), np.isneginf(want_lse))
+        fin = np.isfinite(want_lse)
+        assert np.abs(lse[fin] - want_lse[fin]).max(initial=0.0) <= 2e-3
+
+
+GROUPS = {
+    "one": [(1, [0])],
+    "pair": [(300, [17, 1])],
+    "edges": [(127, [0, 1, 2]), (128, [0, 1]), (129, [130, 0]), (255, [1, 2]), (256, [0, 300]), (257, [1, 255])],
+    "alone": [(0, [5]), (0, [700]), (513, [40])],
+    "idle": [(400, [None, 30, None, 0]), (0, [None]), (200, [None, None]), (640, [64])],
+    "empty": [(77, []), (500, [9, 200]), (0, []), (0, [1, 2, 3])],
+    "many": [(1100, [(7 * i) % 40 for i in range(37)])],
+    "long": [(4000, [3, 500]), (129, [900])],
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups", list(GROUPS))
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (3, 1, 128, 128), (4, 4, 128, 128), (8, 1, 128, 128), (2, 2, 192, 128),
+                                   (4, 2, 256, 256), (5, 1, 256, 256)])
+def test_against_each_agent_alone(shape, groups):
+    f = Forked(shape, GROUPS[groups], seed=31)
+    scale = 1.0 / math.sqrt(shape[2])
+    q = f.q()
+    out, lse = f.run(q, scale)
+    close(out, lse, *f.want(q, scale))
+    assert f.dc.read_flags() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(64, 1, 128, 128), (34, 2, 128, 128), (32, 1, 256, 256), (32, 1, 192, 128), (22, 2, 192, 128)])
+def test_many_query_heads_to_a_kv_head(shape):
+    f = Forked(shape, [(333, [1, 50, 0]), (0, [20])], seed=32)
+    q, scale = f.q(), 1.0 / math.sqrt(shape[2])
+    out, lse = f.run(q, scale)
+    close(out, lse, *f.want(q, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (2, 2, 192, 128), (4, 2, 256, 256)])
+def test_bfloat16_scales_and_bfloat16_output(shape):
+    f = Forked(shape, [(700, [1, 90, 300]), (40, [5])], seed=33, sb_dtype=1, layers=2)
+    q, scale = f.q(), 1.0 / math.sqrt(shape[2])
+    for layer in range(2):
+        out, lse = f.run(q, scale, layer=layer)
+        close(out, lse, *f.want(q, scale, layer))
+        half, none = f.run(q, scale, layer=layer, out_dtype=B.OUT_BF16, want_lse=False)
+        assert torch.equal(half, out.to(torch.bfloat16)) and none is None
+    assert f.dc.read_flags() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(16, 8, 128, 128), (32, 8, 128, 128), (8, 8, 192, 128), (16, 8, 256, 256)])
+def test_references_that_have_to_move(shape):
+    """Scores that climb by thirty binary orders within 512 keys, again and again, with enough keys for several steps to a CTA: the
+    references of the rows' exponentials move, and what was added up before is scaled.  Against the attention over the keys and values
+    as the tiles hold them (each rounded once to binary16): what is left is the rounding of the probabilities, half a step or 2^-11
+    of each, so 2^-11 of the largest value in the numerator and in the denominator, and binary32 sums of scores of magnitude 30
+    (16 * 2^-24 * 30 < 1e-4 in an exponent)."""
+    def climb(f):
+        n = f.lens[0]
+        pos = np.arange(n)
+        blk, slot = f.tables[0][pos // 256], pos % 256
+        for h in range(shape[1]):
+            at = (0, blk, h, slot)
+            x = O.dequantize(O.unpack_codes(f.opool.Kc[at]), f.opool.Ks[at], f.opool.Kb[at]).astype(np.float32)
+            x[:, 0] = (pos % 512) * 0.12 * math.sqrt(shape[2] / 128)
+            c, s, b = O.quantize_rows(synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(x)))
+            f.opool.Kc[at], f.opool.Ks[at], f.opool.Kb[at] = O.pack_codes(c), s, b
+
+    f = Forked(shape, [(20000, [40, 0, 200])], seed=34, edit=climb)
+    qf = synth.bf16_bits_to_f32(f.q())
+    qf[..., 0] = 4.0 + np.abs(qf[..., 0])                # every query has a part along the climbing element
+    q, scale = synth.f32_to_bf16_bits(qf), 1.0 / math.sqrt(shape[2])
+    out, lse = f.run(q, scale)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    qd, rep, most = synth.bf16_bits_to_f32(q).astype(np.float64), shape[0] // shape[1], 0.0
+    for a, n in enumerate(f.lens):
+        for h in range(shape[1]):
+            K, V = (x.astype(np.float16).astype(np.float64) for x in O.gather_dequant(f.opool, 0, f.tables[a], 0, n, h))
+            s = scale * qd[a, h * rep:(h + 1) * rep] @ K.T
+            top = s.max(1, keepdims=True)
+            assert top.max() > 15.0
+            p = np.exp(s - top)
+            want, want_lse = p @ V / p.sum(1, keepdims=True), top[:, 0] + np.log(p.sum(1))
+            assert np.abs(out[a, h * rep:(h + 1) * rep] - want).max() <= 2.0 ** -10 * np.abs(V).max() + 1e-3
+            assert np.abs(lse[a, h * rep:(h + 1) * rep] - want_lse).max() <= 1e-3
+
+
+@pytest.mark.gpu
+def test_one_agents_bad_query_leaves_the_others_alone():
+    f = Forked((8, 2, 128, 128), [(600, [20, 30, 1, 0])], seed=35)
+    q, scale = f.q(), 1.0 / math.sqrt(128)
+    good, _ = f.run(q, scale)
+    bad = q.copy()
+    bad[1, :4] = 0x7F80                                  # infinities
+    bad[1, 4:] = 0x7FC0                                  # NaN
+    bad[3] = synth.f32_to_bf16_bits(synth.bf16_bits_to_f32(bad[3]) * np.float32(1e30))
+    out, _ = f.run(bad, scale)
+    assert torch.equal(out[[0, 2]], good[[0, 2]])
+    tiny = q.copy()
+    tiny[2] = 0
+    out, _ = f.run(tiny, scale)
+    assert torch.equal(out[[0, 1, 3]], good[[0, 1, 3]])
+    close(out, None, *f.want(tiny, scale))
+
+
+@pytest.mark.gpu
+def test_lengths_that_cannot_be_raise_the_flag_and_give_zeros():
+    f = Forked((8, 2, 128, 128), [(300, [20, 30, 9]), (40, [100, 3])], seed=36)
+    q, scale = f.q(), 1.0 / math.sqrt(128)
+    good, good_lse = f.run(q, scale)
+    width = f.tables.shape[1] * 256
+
+    def call(lens=None, offs=None, prefix=None, **kw):
+        f.dc.flags.zero_()
+        out, lse = f.dc.shared_prefix_decode(0, f.lens if lens is None else lens, f.offs if offs is None else offs,
+                                             f.prefix if prefix is None else prefix, q, scale, **kw)
+        return out, lse, f.dc.read_flags()
+
+    def near(x, y, agents):                              # both within ATOL of the truth; the keys may be cut elsewhere
+        return torch.allclose(x[agents], y[agents], rtol=0, atol=2 * ATOL)
+
+    for a, n in ((0, 299), (1, -1), (2, width + 1), (2, 2**31 - 1), (4, 39)):
+        lens = list(f.lens)
+        lens[a] = n
+        out, lse, flag = call(lens=lens)
+        # (another agent leads the first group's prefix when its first one is out: here, one whose row has no entries for it)
+        rest = [i for i in range(5) if i != a] if a else [3, 4]
+        assert flag == (B.FLAG_BAD_LENGTH if a else B.FLAG_BAD_LENGTH | B.FLAG_BAD_BLOCK)
+        assert torch.all(out[a] == 0) and torch.all(torch.isneginf(lse[a])) and near(out, good, rest)
+    out, lse, flag = call(max_kv_len=325)
+    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[1] == 0) and near(out, good, [0, 2, 3, 4])
+    for prefix in ([-1, 40], [width + 1, 40]):
+        out, lse, flag = call(prefix=prefix)
+        assert flag == B.FLAG_BAD_LENGTH and torch.all(out[:3] == 0) and near(out, good, [3, 4])
+    for offs in ([0, 4, 3], [-1, 3, 5], [0, 3, 6], [0, 3, 2**31 - 1], [5, 3, 0]):
+        out, lse, flag = call(offs=offs)
+        assert flag == B.FLAG_BAD_LENGTH and torch.all(out == 0) and torch.all(torch.isneginf(lse)), offs
+    out, lse, flag = call(offs=[0, 3, 4])                # the last agent belongs to no group
+    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[4] == 0) and near(out, good, [0, 1, 2, 3])
+    out, lse, flag = call(offs=[3, 3, 5])
+    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[:3] == 0)
+    out, lse, flag = call()
+    assert flag == 0 and torch.equal(out, good) and torch.equal(lse, good_lse)
+
+
+@pytest.mark.gpu
+def test_bad_blocks_spoil_the_group_or_the_agent():
+    f = Forked((8, 2, 128, 128), [(600, [20, 300, 9]), (40, [100, 3])], seed=37)
+    q, scale = f.q(), 1.0 / math.sqrt(128)
+    good, _ = f.run(q, scale)
+    keep = f.dc.tables.clone()
+    for bad in (-1, f.n_blocks, 2**31 - 1, -2**31):
+        f.dc.tables.copy_(keep)
+        f.dc.tables[0, 1] = bad                          # read for the whole group
+        out, lse = f.run(q, scale)
+        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[:3] == 0) and torch.all(torch.isneginf(lse[:3]))
+        assert torch.equal(out[3:], good[3:])
+        f.dc.flags.zero_()
+        f.dc.tables.copy_(keep)
+        f.dc.tables[1, 3] = bad
+        out, lse = f.run(q, scale)
+        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[1] == 0) and torch.equal(out[[0, 2, 3, 4]], good[[0, 2, 3, 4]])
+        f.dc.flags.zero_()
+
+
+@pytest.mark.gpu
+def test_the_largest_batch_and_runs_that_repeat():
+    """512 agents in uneven groups; the same bits every time, from a workspace that other calls have used, eager and replayed."""
+    r = np.random.default_rng(4)
+    sizes = [200, 1, 100, 64, 33, 114]
+    f = Forked((2, 1, 128, 128), [(int(r.integers(0, 700)), [int(x) for x in r.integers(0, 60, n)]) for n in sizes], seed=38)
+    q, scale = f.q(), 1.0 / math.sqrt(128)
+    out, lse = f.run(q, scale)
+    close(out, lse, *f.want(q, scale))
+    A, spec, dc = 512, f.dc.spec, f.dc
+    need = max(B.q4kv_workspace_bytes_shared_prefix(spec, A, 1024, 6), B.q4kv_workspace_bytes(spec, A, 1024, 0))
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    ws[:B.WORKSPACE_HEADER_BYTES] = 0
+    from paper_2603_04428_b200 import harness as H
+    lens, offs, pre, qd = H.dev(np.asarray(f.lens, np.int32)), H.dev(f.offs), H.dev(np.asarray(f.prefix, np.int32)), H.bf16_dev(q)
+    o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+
+    def call():
+        B.q4kv_shared_prefix_decode_attention(spec, dc.pool, f.n_blocks, 0, dc.bt, lens, 1024, offs, pre, 6, qd, scale, o2, B.OUT_F32,
+                                              l2, ws, dc.flags)
+    call()
+    assert torch.equal(o2, out) and torch.equal(l2, lse) and int(ws[:B.WORKSPACE_HEADER_BYTES].max()) == 0
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for _ in range(3):
+            call()
+    ws.fill_(0xFF)
+    o2.fill_(9.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(o2, out) and torch.equal(l2, lse)
+    gone = torch.arange(A, device="cuda") % 3 == 0       # the replay reads the lengths of the moment
+    gone[f.offs[:-1]] = False                            # (the groups' first agents stay: only their rows hold the prefix here)
+    lens.copy_(torch.where(gone, 0, lens))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.all(o2[gone] == 0) and torch.allclose(o2[~gone], out[~gone], rtol=0, atol=2 * ATOL)
+    assert dc.read_flags() == 0
+
+
+@pytest.mark.gpu
+def test_a_decode_step_of_forked_agents():
+    """Fork, copy, norm and rotate, append, attend: the step as it is used, against agents that hold everything themselves."""
+    from paper_2603_04428_b200 import harness as H
+    hq, hkv, d, n_blocks, parent_len, steps = 8, 2, 128, 24, 700, 3
+    al = B.Allocator(n_blocks)
+    tables = np.full((5, 4), -1, np.int32)
+    tables[0] = al.reserve(0, parent_len, 4)
+    cache = H.DeviceCache(1, hq, hkv, d, d, False, n_blocks, tables)
+    f = torch.from_numpy((10000.0 ** (-2.0 * np.arange(64) / 128)).astype(np.float32)).cuda()
+    w = torch.from_numpy(synth.bf16_bits_to_f32(synth.normal_bf16(6, 1, (2, d)))).cuda().to(torch.bfloat16)
+    how = B.NormRotation.make(norm_dim=d, q_weight=w[0], k_weight=w[1], weight_offset=1.0, rot_dim=d, inv_freq=f)
+
+    def rows(c, bt, pos, offs, qkv):
+        n = qkv.shape[0]
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:].contiguous()
+        qo, ko = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda"), torch.empty((n, hkv, d), dtype=torch.bfloat16, device="cuda")
+        B.q4kv_norm_rope(c.spec, how, len(pos), pos, offs, n, q, k, qo, ko, c.flags)
+        B.q4kv_quantize_append(c.spec, c.pool, c.n_blocks, 0, bt, pos, offs, n, ko, v, c.flags)
+        return qo
+
+    def ints(x):
+        return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+    prompt = H.bf16_dev(synth.normal_bf16(6, 2, (parent_len, hq + 2 * hkv, d)))
+    keep, bt0 = cache.sub_batch(0, 1)
+    rows(cache, bt0, ints([0]), ints([0, parent_len]), prompt)
+    copies = []
+    for child in range(1, 5):
+        tables[child], copy = al.fork(0, child, parent_len, 4)
+        copies.append(copy)
+    B.q4kv_copy_blocks(cache.spec, cache.pool, n_blocks, cache.pool, n_blocks, 0, 1, ints(copies), 4, cache.flags)
+    for a in range(5):
+        tables[a] = al.reserve(a, parent_len + steps, 4)
+    cache.tables.copy_(torch.from_numpy(tables))
+    alone = H.DeviceCache(1, hq, hkv, d, d, False, 20, np.arange(20, dtype=np.int32).reshape(5, 4)[:, ::-1].copy())
+    rows(alone, alone.bt, ints([0] * 5), ints([parent_len * i for i in range(6)]), prompt.repeat(5, 1, 1))
+    for step in range(steps):
+        new = H.bf16_dev(synth.normal_bf16(6, 10 + step, (5, hq + 2 * hkv, d)))
+        pos, offs = ints([parent_len + step] * 5), ints(range(6))
+        q1, q2 = rows(cache, cache.bt, pos, offs, new), rows(alone, alone.bt, pos, offs, new)
+        assert torch.equal(q1, q2)
+        lens = [parent_len + step + 1] * 5
+        out, lse = cache.shared_prefix_decode(0, lens, [0, 5], [parent_len], q1, 1 / math.sqrt(d))
+        ref, ref_lse = alone.decode(0, lens, 0, q2, 1 / math.sqrt(d))
+        close(out, lse, ref.double().cpu().numpy(), ref_lse.double().cpu().numpy())
+    for a in range(5):
+        assert torch.equal(cache.pack(a, parent_len + steps), alone.pack(a, parent_len + steps))
+    assert cache.read_flags() == alone.read_flags() == 0
+
+
+def test_refusals():
+    if torch.cuda.is_available():
+        pytest.skip("placeholder pointers are only handed to the library on a host without a CUDA device")
+    lib, p = B.lib(), 0x1000
+    spec = B.Spec.make(2, 8, 2, 128, 128)
+
+    def call(sp=spec, agents=2, max_blocks=4, pool=p, n_blocks=4, layer=0, lens=p, max_kv=1024, offs=p, prefix=p, groups=1, q=p,
+             scale=0.1, out=p, out_dtype=0, ws=p, size=1 << 40, tables=p):
+        bt = B.Batch(agents, max_blocks, tables)
+        return lib.q4kv_shared_prefix_decode_attention(ctypes.byref(sp), pool, n_blocks, layer, ctypes.byref(bt), lens, max_kv, offs,
+                                                       prefix, groups, q, scale, out, out_dtype, None, ws, size, None, None)
+
+    for bad in (dict(agents=-1), dict(max_blocks=0), dict(pool=None), dict(n_blocks=0), dict(layer=2), dict(layer=-1), dict(lens=None),
+                dict(max_kv=-1), dict(offs=None), dict(prefix=None), dict(groups=0), dict(groups=-1), dict(groups=3), dict(q=None),
+                dict(out=None), dict(out_dtype=2), dict(ws=None), dict(tables=None), dict(pool=0x1008), dict(q=0x1004), dict(out=0x1001),
+                dict(ws=0x1008)):
+        assert call(**bad) == B.EINVAL, bad
+    make = B.Spec.make
+    for bad in (dict(sp=make(2, 8, 2, 64, 64)), dict(sp=make(2, 16, 1, 576, 512, True)), dict(sp=make(2, 8, 2, 128, 128, True)),
+                dict(sp=make(2, 130, 2, 128, 128)), dict(sp=make(2, 66, 2, 256, 256)), dict(sp=make(2, 33, 1, 192, 128)),
+                dict(sp=make(2, 8, 2, 128, 128, exact_products=True)), dict(scale=0.0), dict(scale=0.2), dict(scale=-0.1),
+                dict(agents=513), dict(max_blocks=2**23), dict(agents=512, max_blocks=2**22, max_kv=0, sp=make(2, 64, 64, 128, 128))):
+        assert call(**bad) == B.EUNSUPPORTED, bad
+    need = B.q4kv_workspace_bytes_shared_prefix(spec, 2, 1024, 1)
+    assert need > B.WORKSPACE_HEADER_BYTES and call(size=need - 1) == B.EWORKSPACE
+    assert call(agents=0, tables=None) == B.OK
+    for args in ((make(2, 8, 2, 64, 64), 2, 1024, 1), (spec, 513, 1024, 1), (spec, -1, 1024, 1), (spec, 2, -1, 1), (spec, 2, 1024, 3),
+                 (spec, 2, 1024, -1)):
+        assert B.q4kv_workspace_bytes_shared_prefix(*args) == 0
+    assert B.q4kv_workspace_bytes_shared_prefix(spec, 3, 1024, 1) >= need
