@@ -39,6 +39,7 @@ constexpr int kThreads = 20 * 32;
 constexpr int kRegsSoftmax = 144, kRegsOther = 64;       // of the 96 each thread is launched with
 static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + (kThreads - kSoftmaxWarps * 32) * kRegsOther <= kThreads * 96, "");
 constexpr float kGrow = 14.f;                            // probabilities up to 2^14 (binary16 ends at 65504)
+constexpr int kInfo = 8;                                 // segments that the loader may be ahead of the softmax
 constexpr int kSegmentCost = 1;                          // of a segment beside its steps, in steps
 constexpr uint32_t kColS = 0;                            // tensor-memory columns: S^T 2 x kRows, O^T, K^
 
@@ -101,14 +102,14 @@ __device__ inline int cta_of(const Plan& p, int u) { return (int)(((long long)(u
 
 // One CTA's part of a segment.
 struct Segment {
-  bool prefix;
+  int prefix;                                            // 1: a group's prefix, 0: an agent's own tokens
   int agent0, n_agents, lead, head;                      // rows: agents agent0 .. x n_rep heads of KV head `head`; keys: of agent `lead`
   int key0, key1;                                        // the segment's keys
-  int step0, steps;                                      // 128-key steps of this CTA
+  int step0, steps;                                      // 128-key steps of this CTA; steps == 0: there is no more
   int record;
 };
 
-// Walks the segments of the range [u0, u1) in order; every role has its own.
+// Walks the segments of the range [u0, u1) in order.  The loader does, and hands them to the other roles.
 struct Walker {
   const Plan* p;
   int n_groups, n_agents, heads, most, cta, u0, u1;
@@ -145,7 +146,7 @@ struct Walker {
         while (which < n_groups && p->pre_start[which] + tile_head * length() >= p->pre_start[which + 1]) { ++which; tile_head = 0; }
         if (which == n_groups) { in_prefix = false; which = 0; tile_head = -1; continue; }
         start = p->pre_start[which] + tile_head * length();
-        s.prefix = true;
+        s.prefix = 1;
         s.key0 = 0;
         s.key1 = p->prefix[which];
         s.lead = p->lead[which];
@@ -160,7 +161,7 @@ struct Walker {
         while (which < n_agents && p->suf_start[which] + tile_head * length() >= p->suf_start[which + 1]) { ++which; tile_head = 0; }
         if (which == n_agents) return false;
         start = p->suffix_base + p->suf_start[which] + tile_head * length();
-        s.prefix = false;
+        s.prefix = 0;
         s.key0 = p->prefix[p->group[which]];
         s.key1 = p->kv_len[which];
         s.lead = s.agent0 = which;
@@ -262,11 +263,13 @@ struct Smem {
   alignas(128) uint8_t qs[2][Sh::kQueryBytes];                 // [row][dim]: (r%8)*16 + (r/8)*kSboQ + (k/8)*128
   alignas(128) uint8_t prob[2][Sh::kProbBytes];                // [key][row]: (k%8)*16 + (k/8)*128 + (r/8)*2048 + (r%8)*2
   alignas(16) float kappa[2][Sh::kRows];                       // score in log2 units = S * kappa
-  float red_max[4][Sh::kRows], red_sum[4][Sh::kRows], ref[Sh::kRows];
+  // of the two softmax sets: minus the reference of each row, what to scale by when it moves, partial maxima and sums
+  alignas(16) float neg_ref[2][Sh::kRows / 2], factor[2][Sh::kRows / 2], red_max[2][4][Sh::kRows / 2], red_sum[2][4][Sh::kRows / 2];
   alignas(8) uint64_t raw_full[Sh::kRaw], raw_free[Sh::kRaw];
-  uint64_t k_full[2], k_free[2], v_full[Sh::kStagesV], v_free[Sh::kStagesV], s_full[2], p_full[2], p_free[2], q_full[2], q_free[2], drain;
+  uint64_t k_full[2], s_full[2], p_full[2], o_done[2], q_full[2], q_free[2], info_full[kInfo], info_free[kInfo], drain;
+  Segment info[kInfo];
   uint32_t tmem_base;
-  int bad[Sh::kRaw], poisoned[16];                             // poisoned: of the last segments, a bad block among them
+  int bad[Sh::kRaw], poisoned[kInfo];                          // poisoned: a bad block in the segment
   int abort_flag;
   Plan plan;
 };
@@ -278,15 +281,31 @@ __device__ inline bool set_any(int set, bool v) {        // over the 128 threads
   return r != 0;
 }
 __device__ inline void set_sync(int set) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + set) : "memory"); }
-__device__ inline float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
+__device__ inline float warp_max(float v) {             // (a NaN does not count)
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
 }
 __device__ inline float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+// The sums over a warp of kCount columns, lane c (mod kCount) getting column c's: halves change hands, then quarters, ...
+template <int kCount>
+__device__ inline float column_sums(float (&v)[kCount]) {
+  const int lane = threadIdx.x & 31;
+  if (kCount == 16) {
+#pragma unroll
+    for (int c = 0; c < kCount; ++c) v[c] += __shfl_xor_sync(0xffffffffu, v[c], 16);
+  }
+#pragma unroll
+  for (int o = kCount / 2; o > 0; o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int c = 0; c < o; ++c) v[c] = (high ? v[c + o] : v[c]) + __shfl_xor_sync(0xffffffffu, high ? v[c] : v[c + o], o);
+  }
+  return v[0];
 }
 
 template <int G, int Gv, bool kBf>
@@ -302,11 +321,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRaw; ++s) { mbar_init(&sm.raw_full[s], 1); mbar_init(&sm.raw_free[s], 8); sm.bad[s] = 0; }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&sm.k_full[s], 4); mbar_init(&sm.k_free[s], 1);
-      mbar_init(&sm.s_full[s], 1); mbar_init(&sm.p_full[s], 2); mbar_init(&sm.p_free[s], 1);
+      mbar_init(&sm.k_full[s], 4); mbar_init(&sm.s_full[s], 1); mbar_init(&sm.p_full[s], 6); mbar_init(&sm.o_done[s], 1);
       mbar_init(&sm.q_full[s], 64); mbar_init(&sm.q_free[s], 3);
     }
-    for (int s = 0; s < kStagesV; ++s) { mbar_init(&sm.v_full[s], 4); mbar_init(&sm.v_free[s], 1); }
+    for (int s = 0; s < kInfo; ++s) { mbar_init(&sm.info_full[s], 1); mbar_init(&sm.info_free[s], 2); }
     mbar_init(&sm.drain, 1);
     sm.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -324,27 +342,32 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 4); i += kThreads) reinterpret_cast<int*>(P.plan)[i] = from[i];
   }
   volatile int* abort_flag = &sm.abort_flag;
-  Walker w;
-  w.begin(&sm.plan, P, kRows, blockIdx.x);
-  Segment s;
-  int g = 0, n_seg = 0;                                  // steps and segments so far
+  int g = 0;                                             // steps so far
 
   if (warp >= kLoadWarp) {
     fewer_registers<kRegsOther>();
     if (warp == kLoadWarp) {
-      // =============================== raw steps ==================================================
+      // =============================== segments and raw steps =====================================
       if (lane == 0) {
-        bool ok = true;
-        for (; ok && w.next(s); ++n_seg) {
-          sm.poisoned[n_seg & 15] = 0;
+        Walker w;
+        w.begin(&sm.plan, P, kRows, blockIdx.x);
+        bool more = true;
+        for (int n = 0; more; ++n) {
+          Segment s;
+          more = w.next(s);
+          if (!more) s.steps = 0;
+          if (n >= kInfo && !mbar_wait(&sm.info_free[n % kInfo], (uint32_t)(n / kInfo - 1), abort_flag)) break;
+          sm.info[n % kInfo] = s;
+          sm.poisoned[n % kInfo] = 0;
+          mbar_arrive(&sm.info_full[n % kInfo]);
           const uint8_t* row = head_block(P.pool, y, P.layer, 0, s.head);
           for (int j = 0; j < s.steps; ++j, ++g) {
             const int r = g % kRaw, step = s.step0 + j;
-            if (g >= kRaw && !mbar_wait(&sm.raw_free[r], (uint32_t)(g / kRaw - 1), abort_flag)) { ok = false; break; }
+            if (g >= kRaw && !mbar_wait(&sm.raw_free[r], (uint32_t)(g / kRaw - 1), abort_flag)) { more = false; break; }
             const int blk = P.tables[(size_t)s.lead * P.max_blocks + (step >> 1)];
             sm.bad[r] = blk < 0 || blk >= P.n_blocks;
             if (sm.bad[r]) {
-              sm.poisoned[n_seg & 15] = 1;
+              sm.poisoned[n % kInfo] = 1;
               raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
               mbar_arrive(&sm.raw_full[r]);
             } else {
@@ -360,75 +383,78 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       }
     } else if (warp == kMmaWarp) {
       // =============================== products ===================================================
+      // A product's commit also covers what was issued before it: S^T of a step implies O^T of the step two before, so neither the
+      // buffers of P^T nor those of S^T and K^ need barriers of their own.  The value tile's warps arrive where the softmax does.
       auto wait = [&](uint64_t* bar, int use) {
         const bool ok = mbar_spin(bar, (uint32_t)use, abort_flag);
         if (ok) fence_after_sync();
         return ok;
       };
-      auto issue_pv = [&](int h, int n, bool first) {    // O^T (+)= V^T P^T of step h
-        const int sv = h % kStagesV, ps = h & 1;
-        const uint32_t idesc = idesc_f16(128, 16, 0, 1) + ((uint32_t)((n - 16) >> 3) << 17);
-        const uint64_t vd = smem_desc(smem_u32(sm.vhat[sv]), 128, 1024), pd = smem_desc(smem_u32(sm.prob[ps]), 128, 2048);
+      const uint64_t vd0 = smem_desc(smem_u32(sm.vhat[0]), 128, 1024), pd0 = smem_desc(smem_u32(sm.prob[0]), 128, 2048);
+      const uint64_t qd0 = smem_desc(smem_u32(sm.qs[0]), 128, Sh::kSboQ);
+      bool first = true;
+      uint32_t idesc_pv = 0;                             // of the step whose value product is due
+      auto issue_pv = [&](int h) {                       // O^T (+)= V^T P^T of step h
+        const uint64_t vd = vd0 + (uint64_t)((h % kStagesV) * (2 * Sh::kTileV >> 4)), pd = pd0 + (uint64_t)((h & 1) * (Sh::kProbBytes >> 4));
         if (elect_one()) {
 #pragma unroll
           for (int m = 0; m < Dv / 128; ++m)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_f16_ss(tb + Sh::kColO + kRows * m, vd + (uint64_t)((k >> 2) * (Sh::kTileV >> 4) + m * 1024 + (k & 3) * 16), pd + 16 * k, idesc,
+              mma_f16_ss(tb + Sh::kColO + kRows * m, vd + (uint64_t)((k >> 2) * (Sh::kTileV >> 4) + m * 1024 + (k & 3) * 16), pd + 16 * k, idesc_pv,
                          (!first || k > 0) ? 1u : 0u);
-          commit(&sm.v_free[sv]);
-          commit(&sm.p_free[ps]);
+          commit(&sm.o_done[h & 1]);
         }
         __syncwarp();
       };
-      bool ok = true, first_pv = true;
-      int n_pv = 0;                                      // columns of the step whose value product is due
-      for (; ok && w.next(s); ++n_seg) {
-        const int n = (s.n_agents * y.n_rep + 15) & ~15, slot = n_seg & 1;
-        const uint32_t idesc = idesc_f16(128, 16) + ((uint32_t)((n - 16) >> 3) << 17);
-        ok = wait(&sm.q_full[slot], n_seg >> 1);
-        const uint64_t qd = smem_desc(smem_u32(sm.qs[slot]), 128, Sh::kSboQ);
-        for (int j = 0; ok && j < s.steps; ++j, ++g) {
-          ok = wait(&sm.k_full[g & 1], g >> 1);
-          if (!ok) break;
-          if (elect_one()) {
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
+        const int slot = n & 1;
+        ok = wait(&sm.q_full[slot], n >> 1);
+        const int steps = ok ? sm.info[n % kInfo].steps : 0, columns = ok ? (sm.info[n % kInfo].n_agents * y.n_rep + 15) & ~15 : 0;
+        const uint32_t size = (uint32_t)(columns >> 3) << 17;
+        const uint64_t qd = qd0 + (uint64_t)(slot * (Sh::kQueryBytes >> 4));
+        for (int j = 0; ok && (j < steps || (steps == 0 && j == 0)); ++j) {
+          if (steps > 0) {
+            ok = wait(&sm.k_full[g & 1], g >> 1);
+            if (!ok) break;
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              mma_f16_ts(tb + kColS + kRows * (g & 1), tb + Sh::kColK + (D / 2) * (g & 1) + 8 * k, qd + 16 * k, idesc, k > 0);
-            commit(&sm.s_full[g & 1]);
-            commit(&sm.k_free[g & 1]);
-            if (j == s.steps - 1) commit(&sm.q_free[slot]);
+              for (int k = 0; k < D / 16; ++k)
+                mma_f16_ts(tb + kColS + kRows * (g & 1), tb + Sh::kColK + (D / 2) * (g & 1) + 8 * k, qd + 16 * k, idesc_f16(128, 0) | size, k > 0);
+              commit(&sm.s_full[g & 1]);
+              if (j == steps - 1) commit(&sm.q_free[slot]);
+            }
+            __syncwarp();
           }
-          __syncwarp();
-          if (g > 0) {
-            ok = wait(&sm.v_full[(g - 1) % kStagesV], (g - 1) / kStagesV) && wait(&sm.p_full[(g - 1) & 1], (g - 1) >> 1);
-            if (ok) issue_pv(g - 1, n_pv, first_pv);
+          if (g > 0) {                                   // the step before, also behind the last segment
+            ok = wait(&sm.p_full[(g - 1) & 1], (g - 1) >> 1);
+            if (ok) issue_pv(g - 1);
           }
-          n_pv = n;
-          first_pv = j == 0;
+          first = j == 0;
+          idesc_pv = idesc_f16(128, 0, 0, 1) | size;
+          ++g;
         }
-      }
-      if (ok && g > 0) {
-        ok = wait(&sm.v_full[(g - 1) % kStagesV], (g - 1) / kStagesV) && wait(&sm.p_full[(g - 1) & 1], (g - 1) >> 1);
-        if (ok) issue_pv(g - 1, n_pv, first_pv);
+        if (steps == 0) break;
       }
     } else {
       // =============================== query rows =================================================
       constexpr int kLanes = D == 128 ? 16 : 32, kAtOnce = 8, kStride = 2 * (32 / kLanes);     // lanes of a row, rows in flight, rows of both warps
       const int piece = lane % kLanes, sub = (warp - kQueryWarp) * (32 / kLanes) + lane / kLanes;
-      for (; w.next(s); ++n_seg) {
-        const int slot = n_seg & 1, rows = s.n_agents * y.n_rep, padded = (rows + 15) & ~15;
-        if (n_seg >= 2 && !mbar_wait(&sm.q_free[slot], (uint32_t)((n_seg >> 1) - 1), abort_flag)) break;
+      for (int n = 0;; ++n) {
+        const int slot = n & 1;
+        if (!mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag)) break;
+        const Segment& s = sm.info[n % kInfo];
+        const int steps = s.steps, rows = s.n_agents * y.n_rep, padded = steps > 0 ? (rows + 15) & ~15 : 0;
+        const uint16_t* q = P.q + ((size_t)s.agent0 * y.Hq + (size_t)s.head * y.n_rep) * D + 8 * piece;
+        if (n >= 2 && !mbar_wait(&sm.q_free[slot], (uint32_t)((n >> 1) - 1), abort_flag)) break;
         for (int base = sub; base < padded; base += kStride * kAtOnce) {
           uint4 v[kAtOnce];
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
-            const int r = base + kStride * u;
+            const int r = base + kStride * u, a = r / y.n_rep;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows && piece < D / 8) {
-              const int a = r / y.n_rep;
-              v[u] = *reinterpret_cast<const uint4*>(P.q + ((size_t)(s.agent0 + a) * y.Hq + (size_t)s.head * y.n_rep + (r - a * y.n_rep)) * D + 8 * piece);
-            }
+            if (r < rows && piece < D / 8) v[u] = *reinterpret_cast<const uint4*>(q + ((size_t)a * y.Hq + (r - a * y.n_rep)) * D);
           }
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
@@ -448,6 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         }
         fence_async_smem();
         mbar_arrive(&sm.q_full[slot]);
+        if (steps == 0) break;
       }
     }
   } else if (warp >= kValueWarp) {
@@ -458,31 +485,38 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     const int vr = x7 & 7, vq = (x7 >> 3) & 3, vo = ((vr >> 1) + (x7 >> 5)) & 3;
     const int v_read = Sh::kOffVc + ((vq * 8 + vr) * 4 + vo) * 16, v_write = vr * 16 + (4 * vq) * 1024 + vo * 128;
     const int v_sb = Sh::kOffVsb + (vo * 2 * Gv + (vq >> 1)) * 4;           // + (i * 8 + e) * Gv * 4: token 8 vo + 4 e + i
-    bool go = true;
-    for (; go && w.next(s); ++n_seg) {
-      for (int j = 0; j < s.steps; ++j, ++g) {
+    for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
+      const int key0 = sm.info[n % kInfo].key0, key1 = sm.info[n % kInfo].key1, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+      bool go = steps > 0;
+      for (int j = 0; go && j < steps; ++j, ++g) {
         const int r = g % kRaw, sv = g % kStagesV;
-        if (!mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) ||
-            (g >= kStagesV && !mbar_wait(&sm.v_free[sv], (uint32_t)(g / kStagesV - 1), abort_flag))) { go = false; break; }
+        go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
+             (g < kStagesV || mbar_wait(&sm.o_done[(g - kStagesV) & 1], (uint32_t)((g - kStagesV) >> 1), abort_flag));
+        if (!go) break;
         const bool bad = sm.bad[r] != 0;
         bool over = false;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          const uint8_t* chunk = sm.raw[r] + c * Sh::kChunkBytes;
+          const int at = (step0 + j) * 128 + c * 32, pos = at + 8 * vo;
+          const bool edge = bad || at < key0 || at + 32 > key1;              // some of its bytes are none of the segment's
 #pragma unroll
-        for (int half = 0; half < Gv / 2; ++half) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const uint8_t* chunk = sm.raw[r] + c * Sh::kChunkBytes;
-            const int pos = (s.step0 + j) * 128 + c * 32 + 8 * vo;
+          for (int half = 0; half < Gv / 2; ++half) {
             const uint4 vw = *reinterpret_cast<const uint4*>(chunk + v_read + half * (4 * 8 * 4 * 16));
+            uint32_t e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = *reinterpret_cast<const uint32_t*>(chunk + v_sb + half * 8 + ((i & 3) * 8 + (i >> 2)) * Gv * 4);
+            if (edge) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                if (bad || pos + i < key0 || pos + i >= key1) e[i] = 0u;
+            }
             uint32_t sp[4], bp[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              uint32_t e0 = *reinterpret_cast<const uint32_t*>(chunk + v_sb + half * 8 + i * 8 * Gv * 4);
-              uint32_t e1 = *reinterpret_cast<const uint32_t*>(chunk + v_sb + half * 8 + (i * 8 + 1) * Gv * 4);
-              if (bad || pos + i < s.key0 || pos + i >= s.key1) e0 = 0u;                 // bytes that are none of the segment's
-              if (bad || pos + i + 4 < s.key0 || pos + i + 4 >= s.key1) e1 = 0u;
-              if (kBf) { e0 = bf16_pair_to_h2(e0, over); e1 = bf16_pair_to_h2(e1, over); }
-              sp[i] = __byte_perm(e0, e1, 0x5410);
-              bp[i] = __byte_perm(e0, e1, 0x7632);
+              if (kBf) { e[i] = bf16_pair_to_h2(e[i], over); e[i + 4] = bf16_pair_to_h2(e[i + 4], over); }
+              sp[i] = __byte_perm(e[i], e[i + 4], 0x5410);
+              bp[i] = __byte_perm(e[i], e[i + 4], 0x7632);
             }
             uint8_t* dst = sm.vhat[sv] + v_write + (c >> 1) * Sh::kTileV + (c & 1) * 512 + half * 16384;
             *reinterpret_cast<uint4*>(dst + 0 * 1024) = dequant8(vw.x, sp[0], bp[0], sp[1], bp[1], sp[2], bp[2], sp[3], bp[3], P.masks);
@@ -494,8 +528,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         if (kBf && over) raise_flag(P.flags, Q4KV_FLAG_SB_RANGE);
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) { mbar_arrive(&sm.v_full[sv]); mbar_arrive(&sm.raw_free[r]); }
+        if (lane == 0) { mbar_arrive(&sm.p_full[g & 1]); mbar_arrive(&sm.raw_free[r]); }
       }
+      if (!go) break;
     }
   } else if (warp >= kKeyWarp) {
     fewer_registers<kRegsOther>();
@@ -511,15 +546,17 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       const uint32_t b0 = one ? a3 : a0, b1 = one ? a0 : a1, b2 = one ? a1 : a2, b3 = one ? a2 : a3;
       out[0] = two ? b2 : b0; out[1] = two ? b3 : b1; out[2] = two ? b0 : b2; out[3] = two ? b1 : b3;
     };
-    bool go = true;
-    for (; go && w.next(s); ++n_seg) {
-      for (int j = 0; j < s.steps; ++j, ++g) {
+    for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
+      const int key0 = sm.info[n % kInfo].key0, key1 = sm.info[n % kInfo].key1, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+      bool go = steps > 0;
+      for (int j = 0; go && j < steps; ++j, ++g) {
         const int r = g % kRaw;
-        if (!mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) ||
-            (g >= 2 && !mbar_wait(&sm.k_free[g & 1], (uint32_t)((g >> 1) - 1), abort_flag))) { go = false; break; }
+        go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
+             (g < 2 || mbar_wait(&sm.s_full[g & 1], (uint32_t)((g >> 1) - 1), abort_flag));
+        if (!go) break;
         fence_after_sync();
-        const int pos = (s.step0 + j) * 128 + c * 32 + tau;
-        const bool none = sm.bad[r] != 0 || pos < s.key0 || pos >= s.key1;
+        const int pos = (step0 + j) * 128 + c * 32 + tau;
+        const bool none = sm.bad[r] != 0 || pos < key0 || pos >= key1;
         const uint8_t* raw = sm.raw[r];
         uint32_t sb[G];
         bool over = false;
@@ -565,172 +602,163 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         __syncwarp();
         if (lane == 0) { mbar_arrive(&sm.k_full[g & 1]); mbar_arrive(&sm.raw_free[r]); }
       }
+      if (!go) break;
     }
   } else {
     more_registers<kRegsSoftmax>();
-    // =============================== softmax: a thread has one key and every second group of eight rows ========
-    // (no thread leaves these loops early: after an abort every wait returns at once, and the barriers stay even)
+    // =============================== softmax: a thread has one key and half of the segment's rows ==============
+    // (inside a segment no thread leaves early: after an abort every wait returns at once, and the barriers stay even)
     const int set = warp >> 2, quad = warp & 3;
     const uint32_t lane_addr = tb + ((uint32_t)(quad * 32) << 16);
     const int key = quad * 32 + 8 * (lane >> 3) + elem_of(lane & 7);       // of the step
     const int tid = threadIdx.x & 127;
-    for (; w.next(s); ++n_seg) {
-      const int slot = n_seg & 1, rows = s.n_agents * y.n_rep;
-      const int mine = ((rows + 7) / 8 - set + 1) / 2;                     // groups set, set + 2, ... of eight rows
-      if (quad == set) mbar_spin(&sm.q_full[slot], (uint32_t)(n_seg >> 1), abort_flag);
-      set_sync(set);
-      float ref[8 * kGroups], l[8 * kGroups];
+    float* const neg_ref = sm.neg_ref[set];
+    float* const factor = sm.factor[set];
+    for (int n = 0;; ++n) {
+      const int slot = n & 1;
+      bool lost = false;
+      if (quad == set) lost = !mbar_spin(&sm.q_full[slot], (uint32_t)(n >> 1), abort_flag);
+      if (set_any(set, lost)) break;
+      const Segment s = sm.info[n % kInfo];
+      if (s.steps == 0) break;
+      const int rows = s.n_agents * y.n_rep, first = set * (((rows + 15) & ~15) >> 1);
+      const int mine = min(max((rows - first + 7) >> 3, 0), ((rows + 15) & ~15) >> 4);       // groups of eight rows, from row `first` on
+      const float* kap = sm.kappa[slot] + first;
+      uint64_t l[4 * kGroups];
 #pragma unroll
-      for (int c = 0; c < 8 * kGroups; ++c) { ref[c] = 0.f; l[c] = 0.f; }
-      const float* kap = sm.kappa[slot] + 8 * set;       // + 16 i + c
+      for (int c = 0; c < 4 * kGroups; ++c) l[c] = 0ull;
       bool started = false;
+#pragma unroll 1
       for (int j = 0; j < s.steps; ++j, ++g) {
         const int b = g & 1;
-        if (quad == set) {
-          mbar_spin(&sm.s_full[b], (uint32_t)(g >> 1), abort_flag);
-          if (g >= 2) mbar_spin(&sm.p_free[b], (uint32_t)((g >> 1) - 1), abort_flag);
-        }
+        if (quad == set) mbar_spin(&sm.s_full[b], (uint32_t)(g >> 1), abort_flag);
         set_sync(set);
         fence_after_sync();
         const int pos = (s.step0 + j) * 128 + key;
         const bool valid = pos >= s.key0 && pos < s.key1;
-        const uint32_t s_addr = lane_addr + kColS + kRows * b + 8 * set, o_addr = lane_addr + Sh::kColO + 8 * set;
-        uint8_t* p_at = sm.prob[b] + (quad * 32 + lane) * 16 + set * 2048;
-        float p[8 * kGroups];
-        auto scores = [&](int i) {                       // of group i, in log2 units
-          uint32_t x[8];
-          tmem_ld8(s_addr + 16 * i, x);
-          wait_ld8(x);
-          const float4 k0 = *reinterpret_cast<const float4*>(kap + 16 * i), k1 = *reinterpret_cast<const float4*>(kap + 16 * i + 4);
-          const float kk[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w};
+        const bool edge = (s.step0 + j) * 128 < s.key0 || (s.step0 + j) * 128 + 128 > s.key1;
+        const uint32_t s_addr = lane_addr + kColS + kRows * b + first;
+        uint8_t* const p_at = sm.prob[b] + (quad * 32 + lane) * 16 + (first >> 3) * 2048;
+        uint64_t p[4 * kGroups];
+        bool grown = false;
+#pragma unroll 1
+        for (;;) {
+          if (started) {
+            uint32_t x[8 * kGroups];
+            float most = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) p[8 * i + c] = __uint_as_float(x[c]) * kk[c];
-        };
-        auto probabilities = [&]() {                     // leaves P of the valid keys, reports whether one is too large
-          bool over = false;
+            for (int i = 0; i < kGroups; ++i)
+              if (i < mine) tmem_ld8(s_addr + 8 * i, x + 8 * i);
+            if (kGroups == 4) wait_ld32(x); else wait_ld16(x);
+            if (edge && !valid) {
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i) {
-            if (i < mine) {
-              scores(i);
-              float most = -INFINITY;
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const float t = p[8 * i + c] - ref[8 * i + c];
-                most = fmaxf(most, t);
-                p[8 * i + c] = valid ? fast_exp2(t) : 0.f;
-              }
-              over |= valid && !(most <= kGrow);
-              *reinterpret_cast<uint4*>(p_at + i * 4096) = make_uint4(f32x2_to_h2(p[8 * i], p[8 * i + 1]), f32x2_to_h2(p[8 * i + 2], p[8 * i + 3]),
-                                                                     f32x2_to_h2(p[8 * i + 4], p[8 * i + 5]), f32x2_to_h2(p[8 * i + 6], p[8 * i + 7]));
+              for (int c = 0; c < 8 * kGroups; ++c) x[c] = 0xff800000u;
             }
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+              if (i < mine) {
+                uint32_t h[4];
+#pragma unroll
+                for (int c = 0; c < 4; c += 2) {
+                  const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(kap + 8 * i + 2 * c), rr = *reinterpret_cast<const ulonglong2*>(neg_ref + 8 * i + 2 * c);
+                  const float2 t0 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c]), __uint_as_float(x[8 * i + 2 * c + 1])), kk.x, rr.x));
+                  const float2 t1 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c + 2]), __uint_as_float(x[8 * i + 2 * c + 3])), kk.y, rr.y));
+                  most = fmaxf(fmaxf(most, t0.x), t0.y);
+                  most = fmaxf(fmaxf(most, t1.x), t1.y);
+                  const float a0 = fast_exp2(t0.x), a1 = fast_exp2(t0.y), b0 = fast_exp2(t1.x), b1 = fast_exp2(t1.y);
+                  p[4 * i + c] = pair64(a0, a1);
+                  p[4 * i + c + 1] = pair64(b0, b1);
+                  h[c] = f32x2_to_h2(a0, a1);
+                  h[c + 1] = f32x2_to_h2(b0, b1);
+                }
+                *reinterpret_cast<uint4*>(p_at + i * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
+              }
+            }
+            fence_async_smem();
+            fence_before_sync();
+            if (!set_any(set, most > kGrow) || grown) break;
+          } else if (mine == 0) {
+            break;
           }
-          return over;
-        };
-        bool over = true;
-        if (started) {
-          over = probabilities();
-          fence_async_smem();
-        }
-        if (set_any(set, over && mine > 0)) {
           // the references of the rows that outgrow theirs (of all, in the first step) move to the maximum of this step's scores; the
           // others' stay, so that no row's numbers depend on another's
+#pragma unroll 1
+          for (int i = 0; i < mine; ++i) {
+            uint32_t x[8];
+            tmem_ld8(s_addr + 8 * i, x);
+            wait_ld8(x);
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i) {
-            if (i < mine) {
-              scores(i);
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const float m = warp_max(valid ? p[8 * i + c] : -INFINITY);
-                if (lane == 0) sm.red_max[quad][16 * i + 8 * set + c] = m;
-              }
+            for (int c = 0; c < 8; ++c) {
+              const float m = warp_max(valid ? __uint_as_float(x[c]) * kap[8 * i + c] : -INFINITY);
+              if (lane == 0) sm.red_max[set][quad][8 * i + c] = m;
             }
           }
+          if (started && quad == set) mbar_spin(&sm.o_done[b ^ 1], (uint32_t)((g - 1) >> 1), abort_flag);     // O^T so far is complete
           set_sync(set);
-          if (started && quad == set) mbar_spin(&sm.p_free[b ^ 1], (uint32_t)((g - 1) >> 1), abort_flag);     // O^T so far is complete
-          if (started) set_sync(set);
-          fence_after_sync();
-#pragma unroll
-          for (int i = 0; i < kGroups; ++i) {
-            if (i < mine) {
-              float f[8];
-#pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                const int row = 16 * i + 8 * set + c;
-                const float m = fmaxf(fmaxf(sm.red_max[0][row], sm.red_max[1][row]), fmaxf(sm.red_max[2][row], sm.red_max[3][row]));
-                const float to = started && !(m - ref[8 * i + c] > kGrow) ? ref[8 * i + c] : m;
-                const float next = to > -INFINITY ? to : 0.f;
-                f[c] = fast_exp2(ref[8 * i + c] - next);
-                ref[8 * i + c] = next;
-                l[8 * i + c] *= started ? f[c] : 0.f;
-              }
-              if (started) {
-#pragma unroll
-                for (int m = 0; m < Dv / 128; ++m) {
-                  uint32_t o[8];
-                  tmem_ld8(o_addr + kRows * m + 16 * i, o);
-                  wait_ld8(o);
-#pragma unroll
-                  for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f[c]);
-                  tmem_st8(o_addr + kRows * m + 16 * i, o);
-                }
-              }
-            }
+          if (quad == 0 && lane < 8 * mine) {
+            const float m = fmaxf(fmaxf(sm.red_max[set][0][lane], sm.red_max[set][1][lane]), fmaxf(sm.red_max[set][2][lane], sm.red_max[set][3][lane]));
+            const float old = started ? -neg_ref[lane] : 0.f;
+            const float to = started && !(m - old > kGrow) ? old : m > -INFINITY ? m : 0.f;
+            neg_ref[lane] = -to;
+            factor[lane] = fast_exp2(old - to);
           }
-          if (started) { wait_st(); fence_before_sync(); }
-          probabilities();
-          fence_async_smem();
           set_sync(set);
-          started = true;
+          if (started) {
+            fence_after_sync();
+#pragma unroll
+            for (int i = 0; i < 4 * kGroups; ++i)
+              if (i < 4 * mine) l[i] = mul2(l[i], *reinterpret_cast<const uint64_t*>(factor + 2 * i));
+#pragma unroll 1
+            for (int i = 0; i < mine * (Dv / 128); ++i) {
+              const uint32_t at = lane_addr + Sh::kColO + first + 8 * (i % mine) + kRows * (i / mine);
+              uint32_t o[8];
+              tmem_ld8(at, o);
+              wait_ld8(o);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor[8 * (i % mine) + c]);
+              tmem_st8(at, o);
+            }
+            wait_st();
+            fence_before_sync();
+          }
+          started = grown = true;
         }
         if (tid == 0) mbar_arrive(&sm.p_full[b]);
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i)
-          if (i < mine) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c) l[8 * i + c] += p[8 * i + c];
-          }
+        for (int i = 0; i < 4 * kGroups; ++i)
+          if (i < 4 * mine) l[i] = add2(l[i], p[i]);
       }
       // ---- the segment's record ----
-      if (quad == set) mbar_spin(&sm.p_free[(g - 1) & 1], (uint32_t)((g - 1) >> 1), abort_flag);
+      if (quad == set) mbar_spin(&sm.o_done[(g - 1) & 1], (uint32_t)((g - 1) >> 1), abort_flag);
+      {
+        float v[8 * kGroups];
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i)
-        if (i < mine) {
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const float sum = warp_sum(l[8 * i + c]);
-            if (lane == 0) {
-              sm.red_sum[quad][16 * i + 8 * set + c] = sum;
-              if (quad == 0) sm.ref[16 * i + 8 * set + c] = ref[8 * i + c];
-            }
-          }
-        }
+        for (int i = 0; i < 4 * kGroups; ++i) { const float2 u = unpair64(l[i]); v[2 * i] = u.x; v[2 * i + 1] = u.y; }
+        const float sum = column_sums(v);
+        if (lane < 8 * kGroups) sm.red_sum[set][quad][lane] = sum;
+      }
       if (tid == 0) mbar_arrive(&sm.q_free[slot]);       // the set has passed a barrier since it last read kappa
       set_sync(set);
       fence_after_sync();
-      const bool bad = *abort_flag || sm.poisoned[n_seg & 15];
+      const bool bad = *abort_flag || sm.poisoned[n % kInfo];
       float* o_out = s.prefix ? P.pre_o + (size_t)s.record * Sh::kRecord : P.suf_o + (size_t)s.record * y.n_rep * Dv;
       float2* ml = s.prefix ? P.pre_ml + (size_t)s.record * kRows : P.suf_ml + (size_t)s.record * y.n_rep;
-      if (tid < 8 * mine) {
-        const int row = 16 * (tid >> 3) + 8 * set + (tid & 7);
-        if (row < rows) ml[row] = make_float2(sm.ref[row], bad ? -1.f : sm.red_sum[0][row] + sm.red_sum[1][row] + sm.red_sum[2][row] + sm.red_sum[3][row]);
-      }
+      if (tid < 8 * mine && first + tid < rows)
+        ml[first + tid] = make_float2(-neg_ref[tid], bad ? -1.f : sm.red_sum[set][0][tid] + sm.red_sum[set][1][tid] + sm.red_sum[set][2][tid] + sm.red_sum[set][3][tid]);
+#pragma unroll 1
+      for (int i = 0; i < mine * (Dv / 128); ++i) {
+        const int row = first + 8 * (i % mine), m = i / mine;
+        uint32_t o[8];
+        tmem_ld8(lane_addr + Sh::kColO + row + kRows * m, o);
+        wait_ld8(o);
+        float* at = o_out + (size_t)row * Dv + 128 * m + quad * 32 + lane;
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        if (i < mine) {
-#pragma unroll
-          for (int m = 0; m < Dv / 128; ++m) {
-            uint32_t o[8];
-            tmem_ld8(lane_addr + Sh::kColO + kRows * m + 16 * i + 8 * set, o);
-            wait_ld8(o);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const int row = 16 * i + 8 * set + c;
-              if (row < rows) o_out[(size_t)row * Dv + 128 * m + quad * 32 + lane] = __uint_as_float(o[c]);
-            }
-          }
-        }
+        for (int c = 0; c < 8; ++c)
+          if (row + c < rows) at[c * Dv] = __uint_as_float(o[c]);
       }
       fence_before_sync();
+      set_sync(set);
+      if (tid == 0) mbar_arrive(&sm.info_free[n % kInfo]);
     }
   }
 
