@@ -137,12 +137,15 @@ struct DecodeParams {
   const uint16_t* k_new;      // fused append: bf16 [A][Hkv][D] rows of the token at position kv_len - 1 (null: none)
   const uint16_t* v_new;
   const int32_t* q_offs;      // kSingles: see Params
+  DecodeGroups groups;        // kGroups: see Params
 };
 // kSingles: the batch of a prefill call, in which this launch takes the agents with exactly one query (row q_offs[a]).  An
-// instantiation of its own: the look-ups cost the others 1-4 % as a run-time branch.
-template <bool kSinglesOnly>
+// instantiation of its own: the look-ups cost the others 1-4 % as a run-time branch.  kGroups: the agents of a group leave out the keys of
+// the group's prefix, which another launch attends.
+enum class Batch { kAll, kSingles, kGroups };
+template <Batch kBatch>
 struct Params : DecodeParams {
-  static constexpr bool kSingles = kSinglesOnly;
+  static constexpr bool kSingles = kBatch == Batch::kSingles, kGroups = kBatch == Batch::kGroups;
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -163,8 +166,18 @@ __device__ inline AgentRange agent_range(const Par& P, int a, bool& bad) {
     bad = one && (bad || r.n < 1);
     if (!one) r.n = 0;
   }
-  if (bad) r.n = 0;
-  r.lo = window > 0 ? max(0, r.n - window) : 0;
+  int prefix = 0;
+  if (Par::kGroups) {
+    int g = 0;
+    for (int end = P.groups.n; end - g > 1;) {           // the last group that begins at or before the agent
+      const int mid = (g + end) >> 1;
+      if (P.groups.offs[mid] <= a) g = mid; else end = mid;
+    }
+    prefix = P.groups.prefix_lens[g];
+    bad = bad || P.groups.offs[g] > a || a >= P.groups.offs[g + 1] || prefix < 0 || (r.n > 0 && r.n < prefix);
+  }
+  if (bad) r.n = prefix = 0;
+  r.lo = Par::kGroups ? min(prefix, r.n) : window > 0 ? max(0, r.n - window) : 0;
   r.cf = r.lo >> 5;
   r.nc = r.n > r.lo ? ((r.n + 31) >> 5) - r.cf : 0;
   return r;
@@ -987,8 +1000,9 @@ __device__ __noinline__ uint32_t batch_offsets(const Par& P, const RangeStart& r
   return off;
 }
 
-template <int G, int H, bool kBf, bool kSingles>
-__global__ void __launch_bounds__(warps_of(G) * 32, kCtasPerSm) decode_mma_kernel(const __grid_constant__ Params<kSingles> P) {
+template <int G, int H, bool kBf, Batch kBatch>
+__global__ void __launch_bounds__(warps_of(G) * 32, kCtasPerSm) decode_mma_kernel(const __grid_constant__ Params<kBatch> P) {
+  constexpr bool kSingles = kBatch == Batch::kSingles;
   using S = Smem<G, H>;
   constexpr int NW = S::NW, D = S::D, Gv = S::Gv, Dv = S::Dv, kSlots = S::kSlots, kValSlots = S::kValSlots;
   constexpr bool kHalves = S::kHalves;
@@ -1272,7 +1286,7 @@ __global__ void __launch_bounds__(warps_of(G) * 32, kCtasPerSm) decode_mma_kerne
   }
 }
 
-template <int G, int H, bool kBf, bool kSingles>
+template <int G, int H, bool kBf, Batch kBatch>
 cudaError_t launch_g(const DecodeParams& P_, int grid, cudaStream_t st) {
   static bool configured[64] = {};     // the attributes are per function and device: set them once for each
   constexpr size_t smem = sizeof(Smem<G, H>);
@@ -1281,9 +1295,9 @@ cudaError_t launch_g(const DecodeParams& P_, int grid, cudaStream_t st) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(decode_mma_kernel<G, H, kBf, kSingles>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(decode_mma_kernel<G, H, kBf, kBatch>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(decode_mma_kernel<G, H, kBf, kSingles>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
+    e = cudaFuncSetAttribute(decode_mma_kernel<G, H, kBf, kBatch>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
@@ -1297,14 +1311,15 @@ cudaError_t launch_g(const DecodeParams& P_, int grid, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  Params<kSingles> P;
+  Params<kBatch> P;
   static_cast<DecodeParams&>(P) = P_;
-  return cudaLaunchKernelEx(&cfg, decode_mma_kernel<G, H, kBf, kSingles>, P);
+  return cudaLaunchKernelEx(&cfg, decode_mma_kernel<G, H, kBf, kBatch>, P);
 }
 template <int G, int H>
 cudaError_t launch_gh(const DecodeParams& P, int grid, cudaStream_t st) {
-  if (P.q_offs) return P.y.sb_bf16 ? launch_g<G, H, true, true>(P, grid, st) : launch_g<G, H, false, true>(P, grid, st);
-  return P.y.sb_bf16 ? launch_g<G, H, true, false>(P, grid, st) : launch_g<G, H, false, false>(P, grid, st);
+  if (P.q_offs) return P.y.sb_bf16 ? launch_g<G, H, true, Batch::kSingles>(P, grid, st) : launch_g<G, H, false, Batch::kSingles>(P, grid, st);
+  if (P.groups.n) return P.y.sb_bf16 ? launch_g<G, H, true, Batch::kGroups>(P, grid, st) : launch_g<G, H, false, Batch::kGroups>(P, grid, st);
+  return P.y.sb_bf16 ? launch_g<G, H, true, Batch::kAll>(P, grid, st) : launch_g<G, H, false, Batch::kAll>(P, grid, st);
 }
 
 // Sets of query heads a KV head's heads are cut into: the kernel's columns take four of them, or eight at d = 128
@@ -1356,7 +1371,8 @@ size_t decode_mma_workspace_bytes(const Layout& y, int n_agents, int layer_count
 cudaError_t launch_decode_mma(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b,
                               const int32_t* kv_lens, int max_kv_len, const int32_t* windows, int layer_count,
                               const void* q, float scale, void* out, int out_dtype, float* lse, void* ws, int32_t* flags,
-                              cudaStream_t st, const void* k_new, const void* v_new, const int32_t* q_offs, int32_t* tickets) {
+                              cudaStream_t st, const void* k_new, const void* v_new, const int32_t* q_offs, int32_t* tickets,
+                              const DecodeGroups* groups) {
   if (b.n_agents <= 0 || layer_count <= 0) return cudaSuccess;
   DecodeParams P;
   P.y = y; P.pool = (const uint8_t*)pool; P.n_blocks = n_blocks; P.layer = layer; P.n_agents = b.n_agents * layer_count;
@@ -1377,6 +1393,7 @@ cudaError_t launch_decode_mma(const Layout& y, const void* pool, int n_blocks, i
   P.out = out; P.out_dtype = out_dtype; P.lse = lse; P.flags = flags;
   P.k_new = (const uint16_t*)k_new; P.v_new = (const uint16_t*)v_new;
   P.q_offs = q_offs;
+  P.groups = groups ? *groups : DecodeGroups{nullptr, nullptr, 0};
   // No more CTAs than can be of use: one that finds nothing to do costs the next launch a microsecond, because its CTAs come in as
   // this one's leave.  No fewer than pairs, which one CTA would take in turn: a launch on contexts of 30 tokens took 25.5 us with
   // a CTA per eight chunks, 4.3 with one per pair, on 100 tokens 7.2 and 4.3, at d = 256 13.8 and 6.7.

@@ -137,6 +137,9 @@ cudaError_t launch_attention_generic(const Layout& y, const void* pool, int n_bl
                                      int max_kv_len, int window, const void* q, float scale, void* out,
                                      int out_dtype, float* lse, void* ws, int32_t* flags, cudaStream_t st);
 
+// Agents that share prefixes: group g holds agents offs[g] .. offs[g + 1] - 1 (device memory)
+struct DecodeGroups { const int32_t *offs, *prefix_lens; int n; };
+
 // tensor-core decode path (GQA shapes with d_qk = d_v in {128, 256}, and d_qk 192 with d_v 128)
 bool decode_mma_supported(const Layout& y);
 bool decode_mma_fits(const Layout& y, int n_agents, int max_blocks, int layer_count = 1);
@@ -147,7 +150,9 @@ cudaError_t launch_decode_mma(const Layout& y, const void* pool, int n_blocks, i
                               const void* q, float scale, void* out, int out_dtype, float* lse, void* ws, int32_t* flags,
                               cudaStream_t st, const void* k_new = nullptr, const void* v_new = nullptr,
                               // q_offs: only the agents with exactly one query row; tickets: counters of their own
-                              const int32_t* q_offs = nullptr, int32_t* tickets = nullptr);
+                              const int32_t* q_offs = nullptr, int32_t* tickets = nullptr,
+                              // groups: the keys before an agent's group's prefix_lens are left out
+                              const DecodeGroups* groups = nullptr);
 int decode_mma_tickets(const Layout& y, int n_agents);
 
 // What a tcgen05 prefill launch does beside the attention of its tiles
@@ -201,11 +206,11 @@ cudaError_t launch_merge_prefill(const Layout& y, int total_q, int n_splits, con
                                  const int32_t* q_offs = nullptr, int n_agents = 0);
 
 // Decode of agents that share prefixes (d_qk = d_v in {128, 256}, d_qk 192 / d_v 128)
-bool shared_prefix_supported(const Layout& y, int n_agents, int max_kv_len);
+bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int max_kv_len);
 size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups);
 cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
                                  int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
-                                 float scale, void* out, int out_dtype, float* lse, void* ws, int32_t* flags, cudaStream_t st);
+                                 float scale, void* out, int out_dtype, float* lse, void* workspace, int32_t* flags, cudaStream_t st);
 
 // Decode on the MLA-latent cache (d_qk 576, d_v 512 aliasing K, one KV head, at most 16 query heads): a key-split
 // attention kernel -- on a binary16 tile of the dequantized keys, or, with on_codes, on the 4-bit codes themselves

@@ -1,27 +1,29 @@
 // q4kv_shared_prefix_decode_attention: one query per agent over its whole cache, where groups of agents share a prefix whose keys
 // are read and expanded once for the group (Section 3.4 decode; forked agents, q4kv_allocator_fork).
 //
-//   With the keys of an agent cut into parts i (pieces of the prefix, pieces of its own tokens), part i leaves
+//   With the keys of an agent cut into parts i (pieces of the prefix, its own tokens), part i leaves
 //   m_i = a reference for its scores, l_i = sum 2^(s - m_i), o_i = sum 2^(s - m_i) v, and
 //   out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i with M = max m_i.
 //
-// The work is a list of segments: (group, tile of agents, KV head) over the prefix with up to kMaxRows score rows, then (agent, KV
-// head) over its own tokens with n_rep rows.  The list is cut into equal contiguous ranges of 128-key steps, one per CTA and one CTA
-// per SM; every CTA leaves a record per segment it touched and a second kernel combines an agent's records.
+// Three launches: the prefixes (here), the agents' own tokens (decode_mma, its range beginning behind the prefix), the sum of the parts
+// (here).
 //
-// One step is two products on the fifth-generation tensor cores with the KEYS as the 128 rows, so that the number of query rows is
-// the free dimension N (16 .. 64) and few rows cost little:
+// The prefixes' work is a list of segments (group, tile of agents, KV head) with up to kRows score rows each, cut into equal contiguous
+// ranges of 128-key steps, one per CTA and one CTA per SM; every CTA leaves a record per segment that it touched.  One step is two
+// products on the fifth-generation tensor cores with the KEYS as the 128 rows, so that the number of query rows is the free
+// dimension N (16 .. 64) and few rows cost little:
 //   S^T [128 keys][N] = K^ [128][d_qk] Q^T      K^ (binary16, expanded from the codes) in tensor memory, Q in shared memory
 //   O^T [d_v][N]     += V^T [d_v][128] P^T      V^ and P^T (binary16) in shared memory
 // A lane of tensor memory is a key: a warp that expands keys writes its own lanes (no shared-memory tile, no bank conflicts), and a
-// softmax thread has one key and all rows; masks are a matter of whole lanes.  The sums l stay in the threads' registers until the
-// segment ends.  What a step costs an SM: HBM 790 clocks at d = 128 (18.4 KB), tensor pipe 512 at N = 64.
-//   * A warp streams raw steps into a ring by bulk copies; two warps stage the query rows of the next segment (bf16 times a power of
-//     two per row into binary16, exact).
-//   * Four warps expand keys, four expand values (dequant8: one binary16 fma per pair, each value rounded once).
-//   * Two sets of four softmax warps share the rows, eight at a time.  The reference m of a row is the maximum over the segment's
-//     first step; it moves when a probability would exceed 2^kGrow, which is found by all keys of a set together at the barrier
-//     that also ends the set's stores of P.
+// softmax thread has one key and all rows; the mask is a matter of whole lanes.  The sums l stay in the threads' registers until the
+// segment ends.  What a step costs an SM at d = 128: HBM 790 clocks (18.4 KB), tensor pipe 512 at N = 64.
+//   * A warp walks the list and streams raw steps into a ring by bulk copies; two warps stage the query rows of the next segment
+//     (bf16 times a power of two per row into binary16, exact).
+//   * Two sets of four warps expand keys, two expand values (dequant8: one binary16 fma per pair, each value rounded once), a set
+//     every second step: a step is some 300 instructions for a warp, and a warp alone gets one in about seven clocks.
+//   * Two sets of four softmax warps share the rows.  The reference m of a row is the score of the segment's first key; it moves when a
+//     probability would exceed 2^kGrow, which is found by all keys of a set together at the barrier that also ends the set's
+//     stores of P.
 // All waits are bounded; one that runs out raises Q4KV_FLAG_INTERNAL, lets the copies and the tensor pipe drain and gives the
 // tensor memory back.
 #include "prefill_common.cuh"
@@ -33,11 +35,10 @@ namespace {
 using namespace tc;
 using namespace prefill;
 
-constexpr int kMaxAgents = 512;
-constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 12, kLoadWarp = 16, kMmaWarp = 17, kQueryWarp = 18;
-constexpr int kThreads = 20 * 32;
-constexpr int kRegsSoftmax = 144, kRegsOther = 64;       // of the 96 each thread is launched with
-static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + (kThreads - kSoftmaxWarps * 32) * kRegsOther <= kThreads * 96, "");
+constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 16, kLoadWarp = 24, kMmaWarp = 25, kQueryWarp = 26;
+constexpr int kThreads = 28 * 32;
+constexpr int kRegsSoftmax = 112, kRegsOther = 56;       // of the 72 each thread is launched with
+static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + (kThreads - kSoftmaxWarps * 32) * kRegsOther <= kThreads * 72, "");
 constexpr float kGrow = 14.f;                            // probabilities up to 2^14 (binary16 ends at 65504)
 constexpr int kInfo = 8;                                 // segments that the loader may be ahead of the softmax
 constexpr int kSegmentCost = 1;                          // of a segment beside its steps, in steps
@@ -56,15 +57,7 @@ struct Shape {
   static constexpr int kSboQ = (D / 8) * 128;
   static constexpr uint32_t kColO = 2 * kRows, kColK = kColO + kRows * (Dv / 128);         // K^: two stages of D / 2 columns
   static_assert(kColK + D <= 512, "");
-  static constexpr int kRecord = kRows * Dv;             // floats of a prefix record's o
-};
-
-// What the work list looks like; the merge reads the copy that the first CTA leaves in the workspace.
-struct Plan {
-  int total, n_cta, suffix_base;                         // cost of the whole list, CTAs it is cut for, where the agents' own parts begin
-  int pre_start[kMaxAgents + 1], prefix[kMaxAgents], lead[kMaxAgents], offs[kMaxAgents + 1], tile0[kMaxAgents];   // per group
-  int suf_start[kMaxAgents + 1], kv_len[kMaxAgents];     // per agent; 0: nothing to attend
-  short group[kMaxAgents];
+  static constexpr int kRecord = kRows * Dv;             // floats of a record's o
 };
 
 struct Params {
@@ -77,183 +70,64 @@ struct Params {
   const int32_t* group_offs;
   const int32_t* prefix_lens;
   int n_groups;
+  int grid;                   // of the launch over the prefixes
   const uint16_t* q;
   float scale_log2;
   void* out;
   int out_dtype;
   float* lse;
   int32_t* flags;
-  Plan* plan;
-  float* pre_o;               // [record][row][d_v]
-  float2* pre_ml;             // [record][row]
-  float* suf_o;               // [record][n_rep][d_v]
-  float2* suf_ml;
+  float* rec_o;               // [record][row][d_v]
+  float2* rec_ml;             // [record][row]: m, l
+  const float* own_o;         // [agent][query head][d_v]: of the agents' own tokens, normalised
+  const float* own_lse;       // [agent][query head]
   CodeMasks masks;
 };
 
-__host__ __device__ inline int steps_of(int prefix) { return (prefix + 127) >> 7; }
-__host__ __device__ inline int own_steps(int kv_len, int prefix) { return kv_len > prefix ? ((kv_len + 127) >> 7) - (prefix >> 7) : 0; }
-__device__ inline int cost_of(int steps) { return steps > 0 ? steps + kSegmentCost : 0; }
-// agents of a tile: at most `most`, the tiles of a group as equal as can be
-__host__ __device__ inline int tiles_of(int agents, int most) { return (agents + most - 1) / most; }
-__device__ inline int cut(const Plan& p, int c) { return (int)((long long)p.total * c / p.n_cta); }
-// the CTA whose range holds position u of the list
-__device__ inline int cta_of(const Plan& p, int u) { return (int)(((long long)(u + 1) * p.n_cta - 1) / p.total); }
+// ---- the work list: positions count steps, and kSegmentCost for each segment ----
+struct Group { int agent0, n, prefix, steps, tiles, cost; };   // cost: of one segment
+template <int kRows>
+__device__ inline Group group_of(const Params& P, int g, bool* fine = nullptr) {
+  Group q = {0, 0, 0, 0, 0, 0};
+  if (g < P.n_groups) {
+    const int lo = P.group_offs[g], hi = P.group_offs[g + 1], prefix = P.prefix_lens[g];
+    const bool ok = lo >= 0 && lo <= hi && hi <= P.n_agents;
+    if (fine) *fine = ok;
+    if (ok && prefix >= 0 && prefix <= P.max_kv_len) {
+      q.agent0 = lo;
+      q.n = hi - lo;
+      q.prefix = prefix;
+      q.steps = (prefix + 127) >> 7;
+      const int most = kRows / P.y.n_rep;
+      q.tiles = (q.n + most - 1) / most;                 // as equal as can be: tile t has agents n t / tiles .. n (t + 1) / tiles - 1
+      q.cost = q.tiles > 0 && q.steps > 0 ? q.steps + kSegmentCost : 0;
+    }
+  }
+  return q;
+}
+__device__ inline int inclusive_sum(int v) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+// The list is cut for n CTAs; a CTA's range begins at cut(), cta_of() is the CTA whose range holds position u.
+struct Cut {
+  int total, n;
+  __device__ Cut(int total_, int grid) : total(total_), n(min(grid, max(1, total_))) {}
+  __device__ int begin(int c) const { return (int)((long long)total * c / n); }
+  __device__ int cta_of(int u) const { return (int)(((long long)(u + 1) * n - 1) / total); }
+};
 
-// One CTA's part of a segment.
+// One CTA's part of a segment.  Records are named segment + CTA: both are in order, so no two parts share one.
 struct Segment {
-  int prefix;                                            // 1: a group's prefix, 0: an agent's own tokens
-  int agent0, n_agents, lead, head;                      // rows: agents agent0 .. x n_rep heads of KV head `head`; keys: of agent `lead`
-  int key0, key1;                                        // the segment's keys
-  int step0, steps;                                      // 128-key steps of this CTA; steps == 0: there is no more
+  int agent0, rows, lead, head;                          // rows: agents agent0 .. x n_rep heads of KV head `head`; keys: of agent `lead`
+  int prefix, step0, steps;                              // keys of the prefix; 128-key steps of this CTA (0: there is no more)
   int record;
 };
-
-// Walks the segments of the range [u0, u1) in order.  The loader does, and hands them to the other roles.
-struct Walker {
-  const Plan* p;
-  int n_groups, n_agents, heads, most, cta, u0, u1;
-  int which, tile_head;                                  // group or agent, and (tile, head) or head in it
-  bool in_prefix;
-  __device__ void begin(const Plan* plan, const Params& P, int max_rows, int c) {
-    p = plan;
-    n_groups = P.n_groups; n_agents = P.n_agents; heads = P.y.Hkv; most = max_rows / P.y.n_rep;
-    cta = c;
-    u0 = c < p->n_cta ? cut(*p, c) : 0;
-    u1 = c < p->n_cta ? cut(*p, c + 1) : 0;
-    in_prefix = u0 < p->suffix_base;
-    const int* start = in_prefix ? p->pre_start : p->suf_start;
-    const int at = in_prefix ? u0 : u0 - p->suffix_base;
-    int lo = 0, hi = in_prefix ? n_groups : n_agents;    // the last entry that begins at or before the position
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (start[mid] <= at) lo = mid; else hi = mid;
-    }
-    which = lo;
-    const int len = length();
-    tile_head = len > 0 ? (at - start[which]) / len - 1 : -1;              // next() begins with a step forward
-  }
-  __device__ int length() const {
-    return in_prefix ? (p->pre_start[which + 1] > p->pre_start[which] ? cost_of(steps_of(p->prefix[which])) : 0)
-                     : (p->suf_start[which + 1] - p->suf_start[which]) / heads;
-  }
-  __device__ bool next(Segment& s) {
-    if (u0 >= u1) return false;
-    for (;;) {
-      ++tile_head;
-      int start;
-      if (in_prefix) {
-        while (which < n_groups && p->pre_start[which] + tile_head * length() >= p->pre_start[which + 1]) { ++which; tile_head = 0; }
-        if (which == n_groups) { in_prefix = false; which = 0; tile_head = -1; continue; }
-        start = p->pre_start[which] + tile_head * length();
-        s.prefix = 1;
-        s.key0 = 0;
-        s.key1 = p->prefix[which];
-        s.lead = p->lead[which];
-        s.head = tile_head % heads;
-        const int n = p->offs[which + 1] - p->offs[which], t = tile_head / heads, tiles = tiles_of(n, most);
-        const int a = n * t / tiles;
-        s.agent0 = p->offs[which] + a;
-        s.n_agents = n * (t + 1) / tiles - a;
-        s.step0 = 0;
-        s.record = p->tile0[which] * heads + tile_head + cta;
-      } else {
-        while (which < n_agents && p->suf_start[which] + tile_head * length() >= p->suf_start[which + 1]) { ++which; tile_head = 0; }
-        if (which == n_agents) return false;
-        start = p->suffix_base + p->suf_start[which] + tile_head * length();
-        s.prefix = 0;
-        s.key0 = p->prefix[p->group[which]];
-        s.key1 = p->kv_len[which];
-        s.lead = s.agent0 = which;
-        s.n_agents = 1;
-        s.head = tile_head;
-        s.step0 = s.key0 >> 7;
-        s.record = which * heads + tile_head + cta;
-      }
-      if (start >= u1) return false;
-      const int all = s.prefix ? steps_of(s.key1) : own_steps(s.key1, s.key0);
-      const int first = max(0, u0 - start), last = min(all, u1 - start);
-      if (first >= last) continue;                       // this CTA's part is the segment's fixed cost
-      s.step0 += first;
-      s.steps = last - first;
-      return true;
-    }
-  }
-};
-
-// The plan in shared memory, by the whole CTA.
-__device__ void make_plan(const Params& P, Plan& p, int max_rows) {
-  const int G = P.n_groups, A = P.n_agents, heads = P.y.Hkv, most = max_rows / P.y.n_rep, tid = threadIdx.x;
-  bool ok = true;
-  for (int g = tid; g <= G; g += blockDim.x) {
-    const int lo = P.group_offs[g];
-    p.offs[g] = lo;
-    ok = ok && lo >= 0 && lo <= A && (g == G || P.group_offs[g + 1] >= lo);
-    if (g < G) {
-      p.prefix[g] = P.prefix_lens[g];
-      p.lead[g] = INT32_MAX;
-    }
-  }
-  ok = __syncthreads_and(ok) != 0;
-  bool bad = false;
-  for (int a = tid; a < A; a += blockDim.x) {
-    int lo = 0, hi = G;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.offs[mid] <= a) lo = mid; else hi = mid;
-    }
-    const int kv = P.kv_lens[a], prefix = p.prefix[lo];
-    const bool fine = ok && G > 0 && p.offs[lo] <= a && a < p.offs[lo + 1] && prefix >= 0 && prefix <= P.max_kv_len && kv >= 0 &&
-                      kv <= P.max_kv_len && (kv == 0 || kv >= prefix);
-    const bool live = fine && kv > 0;
-    bad |= !fine;
-    p.group[a] = (short)(live ? lo : -1);
-    p.kv_len[a] = live ? kv : 0;
-    if (live) atomicMin(&p.lead[lo], a);
-  }
-  if (bad && blockIdx.x == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
-  __syncthreads();
-  const int warp = tid >> 5, lane = tid & 31;
-  if (warp < 2) {                                        // running sums: of the groups' cost and tiles, of the agents' cost
-    const int n = warp == 0 ? G : A;
-    int sum = 0, tiles_sum = 0;
-    for (int base = 0; base < n; base += 32) {
-      const int i = base + lane;
-      int cost = 0, tiles = 0;
-      if (i < n) {
-        if (warp == 0) {
-          const int agents = ok ? p.offs[i + 1] - p.offs[i] : 0;
-          tiles = tiles_of(agents, most);
-          cost = p.lead[i] == INT32_MAX ? 0 : tiles * heads * cost_of(steps_of(p.prefix[i]));
-        } else {
-          cost = p.kv_len[i] > 0 ? heads * cost_of(own_steps(p.kv_len[i], p.prefix[p.group[i]])) : 0;
-        }
-      }
-      int c = cost, t = tiles;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int cu = __shfl_up_sync(0xffffffffu, c, o), tu = __shfl_up_sync(0xffffffffu, t, o);
-        if (lane >= o) { c += cu; t += tu; }
-      }
-      if (i < n) {
-        if (warp == 0) { p.pre_start[i] = sum + c - cost; p.tile0[i] = tiles_sum + t - tiles; }
-        else p.suf_start[i] = sum + c - cost;
-      }
-      sum += __shfl_sync(0xffffffffu, c, 31);
-      tiles_sum += __shfl_sync(0xffffffffu, t, 31);
-    }
-    if (lane == 0) {
-      if (warp == 0) p.pre_start[G] = sum; else p.suf_start[A] = sum;
-    }
-  }
-  __syncthreads();
-  if (tid == 0) {
-    p.suffix_base = p.pre_start[G];
-    p.total = p.suffix_base + p.suf_start[A];
-    p.n_cta = min((int)gridDim.x, max(1, p.total));
-  }
-  __syncthreads();
-}
 
 template <int G, int Gv>
 struct Smem {
@@ -271,7 +145,6 @@ struct Smem {
   uint32_t tmem_base;
   int bad[Sh::kRaw], poisoned[kInfo];                          // poisoned: a bad block in the segment
   int abort_flag;
-  Plan plan;
 };
 
 __device__ inline bool set_any(int set, bool v) {        // over the 128 threads of a softmax set; orders their stores
@@ -331,16 +204,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     fence_async_smem();
   }
   if (warp == kMmaWarp) { tmem_alloc(&sm.tmem_base, 512); tmem_relinquish(); }
-  make_plan(P, sm.plan, kRows);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
   const uint32_t tb = sm.tmem_base;
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // the pool, the queries and the workspace are the preceding kernels' until here
-  if (blockIdx.x == 0) {
-    const int* from = reinterpret_cast<const int*>(&sm.plan);
-    for (int i = threadIdx.x; i < (int)(sizeof(Plan) / 4); i += kThreads) reinterpret_cast<int*>(P.plan)[i] = from[i];
-  }
   volatile int* abort_flag = &sm.abort_flag;
   int g = 0;                                             // steps so far
 
@@ -348,39 +215,99 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     fewer_registers<kRegsOther>();
     if (warp == kLoadWarp) {
       // =============================== segments and raw steps =====================================
-      if (lane == 0) {
-        Walker w;
-        w.begin(&sm.plan, P, kRows, blockIdx.x);
-        bool more = true;
-        for (int n = 0; more; ++n) {
-          Segment s;
-          more = w.next(s);
-          if (!more) s.steps = 0;
-          if (n >= kInfo && !mbar_wait(&sm.info_free[n % kInfo], (uint32_t)(n / kInfo - 1), abort_flag)) break;
+      // (lengths, offsets and block tables are inputs that no kernel writes)
+      int total = 0;
+#pragma unroll 1
+      for (int base = 0; base < P.n_groups; base += 32) {
+        const Group q = group_of<kRows>(P, base + lane);
+        total += __reduce_add_sync(0xffffffffu, q.tiles * y.Hkv * q.cost);
+      }
+      const Cut cut(total, gridDim.x);
+      const bool any = (int)blockIdx.x < cut.n && total > 0;
+      const int u0 = any ? cut.begin(blockIdx.x) : 0, u1 = any ? cut.begin(blockIdx.x + 1) : 0;
+      int first = 0, start = 0, tile0 = 0;               // the group that the range begins in, where that group begins, tiles before it
+      if (any) {
+        int tiles = 0;
+#pragma unroll 1
+        for (int base = 0, before = 0;; base += 32) {
+          const Group q = group_of<kRows>(P, base + lane);
+          const int cost = q.tiles * y.Hkv * q.cost, upto = before + inclusive_sum(cost), t = tiles + inclusive_sum(q.tiles);
+          const unsigned past = __ballot_sync(0xffffffffu, upto > u0);
+          if (past) {
+            const int l = __ffs(past) - 1;
+            first = base + l;
+            start = __shfl_sync(0xffffffffu, upto - cost, l);
+            tile0 = __shfl_sync(0xffffffffu, t - q.tiles, l);
+            break;
+          }
+          before = __shfl_sync(0xffffffffu, upto, 31);
+          tiles = __shfl_sync(0xffffffffu, t, 31);
+        }
+      }
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      int n = 0;                                         // segments handed out
+      bool ok = true;
+      auto hand_out = [&](const Segment& s) {
+        if (n >= kInfo && !mbar_wait(&sm.info_free[n % kInfo], (uint32_t)(n / kInfo - 1), abort_flag)) ok = false;
+        if (ok && lane == 0) {
           sm.info[n % kInfo] = s;
           sm.poisoned[n % kInfo] = 0;
           mbar_arrive(&sm.info_full[n % kInfo]);
-          const uint8_t* row = head_block(P.pool, y, P.layer, 0, s.head);
-          for (int j = 0; j < s.steps; ++j, ++g) {
-            const int r = g % kRaw, step = s.step0 + j;
-            if (g >= kRaw && !mbar_wait(&sm.raw_free[r], (uint32_t)(g / kRaw - 1), abort_flag)) { more = false; break; }
-            const int blk = P.tables[(size_t)s.lead * P.max_blocks + (step >> 1)];
-            sm.bad[r] = blk < 0 || blk >= P.n_blocks;
-            if (sm.bad[r]) {
-              sm.poisoned[n % kInfo] = 1;
-              raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
-              mbar_arrive(&sm.raw_full[r]);
-            } else {
-              mbar_arrive_expect_tx(&sm.raw_full[r], Sh::kRawBytes);
-              bulk_load(sm.raw[r], row + (uint64_t)blk * y.block_bytes + (size_t)(step & 1) * Sh::kRawBytes, Sh::kRawBytes, &sm.raw_full[r]);
+        }
+      };
+#pragma unroll 1
+      for (int gr = first; ok && any && start < u1; ++gr) {
+        const Group q = group_of<kRows>(P, gr);
+        int lead = -1;                                   // the first agent that has the prefix
+#pragma unroll 1
+        for (int base = 0; base < q.n && lead < 0; base += 32) {
+          const int a = q.agent0 + base + lane, kv = base + lane < q.n ? P.kv_lens[a] : -1;
+          const unsigned has = __ballot_sync(0xffffffffu, kv >= q.prefix && kv > 0 && kv <= P.max_kv_len);
+          if (has) lead = q.agent0 + base + __ffs(has) - 1;
+        }
+        const int segments = q.tiles * y.Hkv;
+        int k = q.cost > 0 && u0 > start ? (u0 - start) / q.cost : 0;
+        if (lead < 0 || q.cost == 0) k = segments;
+#pragma unroll 1
+        for (; ok && k < segments; ++k) {
+          const int at = start + k * q.cost;
+          if (at >= u1) break;
+          const int from = max(0, u0 - at), to = min(q.steps, u1 - at);
+          if (from >= to) continue;                      // this CTA's part is the segment's fixed cost
+          const int t = k / y.Hkv, a = q.n * t / q.tiles;
+          Segment s;
+          s.agent0 = q.agent0 + a; s.rows = (q.n * (t + 1) / q.tiles - a) * y.n_rep; s.lead = lead; s.head = k - t * y.Hkv;
+          s.prefix = q.prefix; s.step0 = from; s.steps = to - from; s.record = tile0 * y.Hkv + k + (int)blockIdx.x;
+          hand_out(s);
+          if (lane == 0) {
+            const uint8_t* row = head_block(P.pool, y, P.layer, 0, s.head);
+            for (int j = 0; ok && j < s.steps; ++j, ++g) {
+              const int r = g % kRaw, step = s.step0 + j;
+              if (g >= kRaw && !mbar_wait(&sm.raw_free[r], (uint32_t)(g / kRaw - 1), abort_flag)) { ok = false; break; }
+              const int blk = P.tables[(size_t)s.lead * P.max_blocks + (step >> 1)];
+              sm.bad[r] = blk < 0 || blk >= P.n_blocks;
+              if (sm.bad[r]) {
+                sm.poisoned[n % kInfo] = 1;
+                raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
+                mbar_arrive(&sm.raw_full[r]);
+              } else {
+                mbar_arrive_expect_tx(&sm.raw_full[r], Sh::kRawBytes);
+                bulk_load(sm.raw[r], row + (uint64_t)blk * y.block_bytes + (size_t)(step & 1) * Sh::kRawBytes, Sh::kRawBytes, &sm.raw_full[r]);
+              }
             }
           }
+          ok = __all_sync(0xffffffffu, ok);
+          ++n;
         }
-        // a CTA that is giving up still lets its own copies land before shared memory is released
-        if (*abort_flag)
-          for (int j = max(0, g - kRaw); j < g; ++j)
-            for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(&sm.raw_full[j % kRaw], (uint32_t)(j / kRaw) & 1u); ++i) {}
+        start += segments * q.cost;
+        tile0 += q.tiles;
       }
+      Segment last = {};
+      hand_out(last);
+      // a CTA that is giving up still lets its own copies land before shared memory is released
+      if (lane == 0 && *abort_flag)
+        for (int j = max(0, g - kRaw); j < g; ++j)
+          for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(&sm.raw_full[j % kRaw], (uint32_t)(j / kRaw) & 1u); ++i) {}
     } else if (warp == kMmaWarp) {
       // =============================== products ===================================================
       // A product's commit also covers what was issued before it: S^T of a step implies O^T of the step two before, so neither the
@@ -411,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       for (int n = 0; ok; ++n) {
         const int slot = n & 1;
         ok = wait(&sm.q_full[slot], n >> 1);
-        const int steps = ok ? sm.info[n % kInfo].steps : 0, columns = ok ? (sm.info[n % kInfo].n_agents * y.n_rep + 15) & ~15 : 0;
+        const int steps = ok ? sm.info[n % kInfo].steps : 0, columns = ok ? (sm.info[n % kInfo].rows + 15) & ~15 : 0;
         const uint32_t size = (uint32_t)(columns >> 3) << 17;
         const uint64_t qd = qd0 + (uint64_t)(slot * (Sh::kQueryBytes >> 4));
         for (int j = 0; ok && (j < steps || (steps == 0 && j == 0)); ++j) {
@@ -439,13 +366,14 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       }
     } else {
       // =============================== query rows =================================================
-      constexpr int kLanes = D == 128 ? 16 : 32, kAtOnce = 8, kStride = 2 * (32 / kLanes);     // lanes of a row, rows in flight, rows of both warps
+      constexpr int kLanes = D == 128 ? 16 : 32, kAtOnce = 4, kStride = 2 * (32 / kLanes);     // lanes of a row, rows in flight, rows of both warps
+      asm volatile("griddepcontrol.wait;" ::: "memory");
       const int piece = lane % kLanes, sub = (warp - kQueryWarp) * (32 / kLanes) + lane / kLanes;
       for (int n = 0;; ++n) {
         const int slot = n & 1;
         if (!mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag)) break;
         const Segment& s = sm.info[n % kInfo];
-        const int steps = s.steps, rows = s.n_agents * y.n_rep, padded = steps > 0 ? (rows + 15) & ~15 : 0;
+        const int steps = s.steps, rows = s.rows, padded = steps > 0 ? (rows + 15) & ~15 : 0;
         const uint16_t* q = P.q + ((size_t)s.agent0 * y.Hq + (size_t)s.head * y.n_rep) * D + 8 * piece;
         if (n >= 2 && !mbar_wait(&sm.q_free[slot], (uint32_t)((n >> 1) - 1), abort_flag)) break;
         for (int base = sub; base < padded; base += kStride * kAtOnce) {
@@ -480,15 +408,16 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
   } else if (warp >= kValueWarp) {
     fewer_registers<kRegsOther>();
     // =============================== values into shared memory ==================================
-    const int x7 = threadIdx.x - kValueWarp * 32;
+    const int x7 = threadIdx.x & 127, mine = (warp - kValueWarp) >> 2;       // this set's steps: g % 2 == mine
     // one 16-byte piece (dims 32 vq + 8 k + vr, k = 0..3) of token octet vo of a chunk; at d_v = 256 vq + 4 as well
     const int vr = x7 & 7, vq = (x7 >> 3) & 3, vo = ((vr >> 1) + (x7 >> 5)) & 3;
     const int v_read = Sh::kOffVc + ((vq * 8 + vr) * 4 + vo) * 16, v_write = vr * 16 + (4 * vq) * 1024 + vo * 128;
     const int v_sb = Sh::kOffVsb + (vo * 2 * Gv + (vq >> 1)) * 4;           // + (i * 8 + e) * Gv * 4: token 8 vo + 4 e + i
     for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
-      const int key0 = sm.info[n % kInfo].key0, key1 = sm.info[n % kInfo].key1, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+      const int key1 = sm.info[n % kInfo].prefix, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
       bool go = steps > 0;
       for (int j = 0; go && j < steps; ++j, ++g) {
+        if ((g & 1) != mine) continue;
         const int r = g % kRaw, sv = g % kStagesV;
         go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
              (g < kStagesV || mbar_wait(&sm.o_done[(g - kStagesV) & 1], (uint32_t)((g - kStagesV) >> 1), abort_flag));
@@ -499,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         for (int c = 0; c < 4; ++c) {
           const uint8_t* chunk = sm.raw[r] + c * Sh::kChunkBytes;
           const int at = (step0 + j) * 128 + c * 32, pos = at + 8 * vo;
-          const bool edge = bad || at < key0 || at + 32 > key1;              // some of its bytes are none of the segment's
+          const bool edge = bad || at + 32 > key1;       // some of its bytes are none of the prefix's
 #pragma unroll
           for (int half = 0; half < Gv / 2; ++half) {
             const uint4 vw = *reinterpret_cast<const uint4*>(chunk + v_read + half * (4 * 8 * 4 * 16));
@@ -509,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             if (edge) {
 #pragma unroll
               for (int i = 0; i < 8; ++i)
-                if (bad || pos + i < key0 || pos + i >= key1) e[i] = 0u;
+                if (bad || pos + i >= key1) e[i] = 0u;
             }
             uint32_t sp[4], bp[4];
 #pragma unroll
@@ -537,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     // =============================== keys into tensor memory ====================================
     // Lane l of warp c holds token tau = 8 (l / 8) + elem_of(l % 8) of chunk c, so that lanes follow the order of V^'s keys.  A token's
     // words 16 j + 4 m + t lie in four 16-byte pieces t; lane l begins with piece l / 2 % 4 (no bank conflicts) and turns them back.
-    const int c = warp - kKeyWarp, tau = 8 * (lane >> 3) + elem_of(lane & 7), ti = tau & 3, tg = tau >> 2, rot = (lane >> 1) & 3;
+    const int c = warp & 3, mine = (warp - kKeyWarp) >> 2, tau = 8 * (lane >> 3) + elem_of(lane & 7), ti = tau & 3, tg = tau >> 2, rot = (lane >> 1) & 3;
     const int k_read = c * Sh::kChunkBytes + ti * (256 * G) + tg * 64;      // + j * 512 + piece * 16
     const int k_sb = c * Sh::kChunkBytes + Sh::kOffKsb + ((ti * 4 + (tau >> 3)) * 2 + ((tau >> 2) & 1)) * G * 4;
     const uint32_t lane_addr = tb + ((uint32_t)(c * 32) << 16) + Sh::kColK;
@@ -547,16 +476,17 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       out[0] = two ? b2 : b0; out[1] = two ? b3 : b1; out[2] = two ? b0 : b2; out[3] = two ? b1 : b3;
     };
     for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
-      const int key0 = sm.info[n % kInfo].key0, key1 = sm.info[n % kInfo].key1, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+      const int key1 = sm.info[n % kInfo].prefix, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
       bool go = steps > 0;
       for (int j = 0; go && j < steps; ++j, ++g) {
+        if ((g & 1) != mine) continue;
         const int r = g % kRaw;
         go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
              (g < 2 || mbar_wait(&sm.s_full[g & 1], (uint32_t)((g >> 1) - 1), abort_flag));
         if (!go) break;
         fence_after_sync();
         const int pos = (step0 + j) * 128 + c * 32 + tau;
-        const bool none = sm.bad[r] != 0 || pos < key0 || pos >= key1;
+        const bool none = sm.bad[r] != 0 || pos >= key1;
         const uint8_t* raw = sm.raw[r];
         uint32_t sb[G];
         bool over = false;
@@ -578,15 +508,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           tmem_st16(to + at, col);
         };
 #pragma unroll
-        for (int jj = 0; jj < G / 2; ++jj) {
-          uint4 p[4];
+        for (int jj = 0; jj < G; ++jj) {                 // words 4 (2 jj), 4 (2 jj + 1) + t: half of a piece at a time
+          if (jj < (G & ~1)) {
+            uint2 p[4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) p[t] = *reinterpret_cast<const uint4*>(raw + k_read + jj * 512 + ((t + rot) & 3) * 16);
-          uint32_t wd[4];
-          turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, sb[2 * jj], 64 * jj);
-          turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, sb[2 * jj], 64 * jj + 16);
-          turned(p[0].z, p[1].z, p[2].z, p[3].z, wd); expand(wd, sb[2 * jj + 1], 64 * jj + 32);
-          turned(p[0].w, p[1].w, p[2].w, p[3].w, wd); expand(wd, sb[2 * jj + 1], 64 * jj + 48);
+            for (int t = 0; t < 4; ++t) p[t] = *reinterpret_cast<const uint2*>(raw + k_read + (jj >> 1) * 512 + (jj & 1) * 8 + ((t + rot) & 3) * 16);
+            uint32_t wd[4];
+            turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, sb[jj], 32 * jj);
+            turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, sb[jj], 32 * jj + 16);
+          }
         }
         if (G & 1) {                                     // the last group: 8-byte pieces, words 16 + 4 m + t, m = 0, 1
           uint2 p[4];
@@ -621,89 +551,96 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       if (set_any(set, lost)) break;
       const Segment s = sm.info[n % kInfo];
       if (s.steps == 0) break;
-      const int rows = s.n_agents * y.n_rep, first = set * (((rows + 15) & ~15) >> 1);
+      const int rows = s.rows, first = set * (((rows + 15) & ~15) >> 1);
       const int mine = min(max((rows - first + 7) >> 3, 0), ((rows + 15) & ~15) >> 4);       // groups of eight rows, from row `first` on
       const float* kap = sm.kappa[slot] + first;
       uint64_t l[4 * kGroups];
 #pragma unroll
       for (int c = 0; c < 4 * kGroups; ++c) l[c] = 0ull;
-      bool started = false;
 #pragma unroll 1
       for (int j = 0; j < s.steps; ++j, ++g) {
         const int b = g & 1;
-        if (quad == set) mbar_spin(&sm.s_full[b], (uint32_t)(g >> 1), abort_flag);
-        set_sync(set);
+        mbar_wait(&sm.s_full[b], (uint32_t)(g >> 1), abort_flag);
         fence_after_sync();
-        const int pos = (s.step0 + j) * 128 + key;
-        const bool valid = pos >= s.key0 && pos < s.key1;
-        const bool edge = (s.step0 + j) * 128 < s.key0 || (s.step0 + j) * 128 + 128 > s.key1;
+        const bool edge = (s.step0 + j) * 128 + 128 > s.prefix, valid = (s.step0 + j) * 128 + key < s.prefix;
         const uint32_t s_addr = lane_addr + kColS + kRows * b + first;
         uint8_t* const p_at = sm.prob[b] + (quad * 32 + lane) * 16 + (first >> 3) * 2048;
+        if (j == 0) {                                    // a first reference for every row: the score of the first key
+          if (quad == 0) {
+#pragma unroll 1
+            for (int i = 0; i < mine; ++i) {
+              uint32_t x[8];
+              tmem_ld8(s_addr + 8 * i, x);
+              wait_ld8(x);
+              if (lane == 0) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) neg_ref[8 * i + c] = -(__uint_as_float(x[c]) * kap[8 * i + c]);
+              }
+            }
+          }
+          set_sync(set);
+        }
         uint64_t p[4 * kGroups];
         bool grown = false;
 #pragma unroll 1
         for (;;) {
-          if (started) {
-            uint32_t x[8 * kGroups];
-            float most = -INFINITY;
+          uint32_t x[8 * kGroups];
+          float most = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i)
-              if (i < mine) tmem_ld8(s_addr + 8 * i, x + 8 * i);
-            if (kGroups == 4) wait_ld32(x); else wait_ld16(x);
-            if (edge && !valid) {
+          for (int i = 0; i < kGroups; ++i)
+            if (i < mine) tmem_ld8(s_addr + 8 * i, x + 8 * i);
+          if (kGroups == 4) wait_ld32(x); else wait_ld16(x);
+          if (edge && !valid) {
 #pragma unroll
-              for (int c = 0; c < 8 * kGroups; ++c) x[c] = 0xff800000u;
-            }
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-              if (i < mine) {
-                uint32_t h[4];
-#pragma unroll
-                for (int c = 0; c < 4; c += 2) {
-                  const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(kap + 8 * i + 2 * c), rr = *reinterpret_cast<const ulonglong2*>(neg_ref + 8 * i + 2 * c);
-                  const float2 t0 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c]), __uint_as_float(x[8 * i + 2 * c + 1])), kk.x, rr.x));
-                  const float2 t1 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c + 2]), __uint_as_float(x[8 * i + 2 * c + 3])), kk.y, rr.y));
-                  most = fmaxf(fmaxf(most, t0.x), t0.y);
-                  most = fmaxf(fmaxf(most, t1.x), t1.y);
-                  const float a0 = fast_exp2(t0.x), a1 = fast_exp2(t0.y), b0 = fast_exp2(t1.x), b1 = fast_exp2(t1.y);
-                  p[4 * i + c] = pair64(a0, a1);
-                  p[4 * i + c + 1] = pair64(b0, b1);
-                  h[c] = f32x2_to_h2(a0, a1);
-                  h[c + 1] = f32x2_to_h2(b0, b1);
-                }
-                *reinterpret_cast<uint4*>(p_at + i * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
-              }
-            }
-            fence_async_smem();
-            fence_before_sync();
-            if (!set_any(set, most > kGrow) || grown) break;
-          } else if (mine == 0) {
-            break;
+            for (int c = 0; c < 8 * kGroups; ++c) x[c] = 0xff800000u;
           }
-          // the references of the rows that outgrow theirs (of all, in the first step) move to the maximum of this step's scores; the
-          // others' stay, so that no row's numbers depend on another's
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            if (i < mine) {
+              uint32_t h[4];
+#pragma unroll
+              for (int c = 0; c < 4; c += 2) {
+                const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(kap + 8 * i + 2 * c), rr = *reinterpret_cast<const ulonglong2*>(neg_ref + 8 * i + 2 * c);
+                const float2 t0 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c]), __uint_as_float(x[8 * i + 2 * c + 1])), kk.x, rr.x));
+                const float2 t1 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c + 2]), __uint_as_float(x[8 * i + 2 * c + 3])), kk.y, rr.y));
+                most = fmaxf(fmaxf(most, t0.x), t0.y);
+                most = fmaxf(fmaxf(most, t1.x), t1.y);
+                const float a0 = fast_exp2(t0.x), a1 = fast_exp2(t0.y), b0 = fast_exp2(t1.x), b1 = fast_exp2(t1.y);
+                p[4 * i + c] = pair64(a0, a1);
+                p[4 * i + c + 1] = pair64(b0, b1);
+                h[c] = f32x2_to_h2(a0, a1);
+                h[c + 1] = f32x2_to_h2(b0, b1);
+              }
+              *reinterpret_cast<uint4*>(p_at + i * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+          }
+          fence_async_smem();
+          fence_before_sync();
+          if (!set_any(set, most > kGrow) || grown) break;
+          // the references of the rows that outgrow theirs move to the maximum of this step's scores; the others' stay, so that no row's
+          // numbers depend on another's
+          fence_after_sync();
 #pragma unroll 1
           for (int i = 0; i < mine; ++i) {
-            uint32_t x[8];
-            tmem_ld8(s_addr + 8 * i, x);
-            wait_ld8(x);
+            uint32_t z[8];
+            tmem_ld8(s_addr + 8 * i, z);
+            wait_ld8(z);
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-              const float m = warp_max(valid ? __uint_as_float(x[c]) * kap[8 * i + c] : -INFINITY);
+              const float m = warp_max(valid ? __uint_as_float(z[c]) * kap[8 * i + c] : -INFINITY);
               if (lane == 0) sm.red_max[set][quad][8 * i + c] = m;
             }
           }
-          if (started && quad == set) mbar_spin(&sm.o_done[b ^ 1], (uint32_t)((g - 1) >> 1), abort_flag);     // O^T so far is complete
+          if (j > 0 && quad == set) mbar_spin(&sm.o_done[b ^ 1], (uint32_t)((g - 1) >> 1), abort_flag);       // O^T so far is complete
           set_sync(set);
           if (quad == 0 && lane < 8 * mine) {
             const float m = fmaxf(fmaxf(sm.red_max[set][0][lane], sm.red_max[set][1][lane]), fmaxf(sm.red_max[set][2][lane], sm.red_max[set][3][lane]));
-            const float old = started ? -neg_ref[lane] : 0.f;
-            const float to = started && !(m - old > kGrow) ? old : m > -INFINITY ? m : 0.f;
+            const float old = -neg_ref[lane], to = m - old > kGrow ? m : old;
             neg_ref[lane] = -to;
-            factor[lane] = fast_exp2(old - to);
+            factor[lane] = to == old ? 1.f : fast_exp2(old - to);
           }
           set_sync(set);
-          if (started) {
+          if (j > 0) {
             fence_after_sync();
 #pragma unroll
             for (int i = 0; i < 4 * kGroups; ++i)
@@ -721,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             wait_st();
             fence_before_sync();
           }
-          started = grown = true;
+          grown = true;
         }
         if (tid == 0) mbar_arrive(&sm.p_full[b]);
 #pragma unroll
@@ -741,8 +678,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       set_sync(set);
       fence_after_sync();
       const bool bad = *abort_flag || sm.poisoned[n % kInfo];
-      float* o_out = s.prefix ? P.pre_o + (size_t)s.record * Sh::kRecord : P.suf_o + (size_t)s.record * y.n_rep * Dv;
-      float2* ml = s.prefix ? P.pre_ml + (size_t)s.record * kRows : P.suf_ml + (size_t)s.record * y.n_rep;
+      float* o_out = P.rec_o + (size_t)s.record * Sh::kRecord;
+      float2* ml = P.rec_ml + (size_t)s.record * kRows;
       if (tid < 8 * mine && first + tid < rows)
         ml[first + tid] = make_float2(-neg_ref[tid], bad ? -1.f : sm.red_sum[set][0][tid] + sm.red_sum[set][1][tid] + sm.red_sum[set][2][tid] + sm.red_sum[set][3][tid]);
 #pragma unroll 1
@@ -779,55 +716,74 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
   }
 }
 
-// One warp per (agent, query head): the records of the prefix's parts and of the agent's own, weighted by 2^(m - M).  Bound by the
-// latency of the plan and of the records in L2.
-template <int Dv>
-__global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_constant__ Params P, int max_rows, int record) {
+// One warp per (agent, query head): the records of the prefix's parts and the agent's own tokens, weighted by 2^(m - M).  Bound by
+// the latency of the lengths and of the records in L2.
+template <int Dv, int kRows>
+__global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_constant__ Params P) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31, Hq = P.y.Hq, heads = P.y.Hkv, n_rep = P.y.n_rep;
   const int at = blockIdx.x * 4 + (threadIdx.x >> 5), a = at / Hq, head = at % Hq / n_rep, rep = at % n_rep;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (a >= P.n_agents) return;
-  const Plan& p = *P.plan;
-  const int kv = p.kv_len[a], g = p.group[a];
-  int n_pre = 0, n_own = 0, pre = 0, own = 0, row = 0;   // parts, the first one's record, the row in a prefix record
-  if (kv > 0) {
-    const int prefix = p.prefix[g], steps = steps_of(prefix), mine = own_steps(kv, prefix);
-    if (steps > 0) {
-      const int n = p.offs[g + 1] - p.offs[g], tiles = tiles_of(n, max_rows / n_rep), i = a - p.offs[g];
-      const int t = ((i + 1) * tiles - 1) / n, segment = t * heads + head;
-      const int start = p.pre_start[g] + segment * cost_of(steps), c0 = cta_of(p, start);
-      n_pre = cta_of(p, start + steps - 1) - c0 + 1;
-      pre = p.tile0[g] * heads + segment + c0;
-      row = (i - n * t / tiles) * n_rep + rep;
-    }
-    if (mine > 0) {
-      const int start = p.suffix_base + p.suf_start[a] + head * cost_of(mine), c0 = cta_of(p, start);
-      n_own = cta_of(p, start + mine - 1) - c0 + 1;
-      own = a * heads + head + c0;
-    }
+  if (a >= P.n_agents) {                                 // (or the grid could complete before the one it follows)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
   }
+  // the agent's group, where it begins in the list, and how the list was cut
+  int total = 0, start = 0, tile0 = 0, tiles = 0;
+  bool ascending = true, found = false;
+  Group mine = {0, 0, 0, 0, 0, 0};
+#pragma unroll 1
+  for (int base = 0; base < P.n_groups; base += 32) {
+    bool fine = true;
+    const Group q = group_of<kRows>(P, base + lane, &fine);
+    ascending = ascending && __all_sync(0xffffffffu, fine);
+    const int cost = q.tiles * heads * q.cost, upto = total + inclusive_sum(cost), t = tiles + inclusive_sum(q.tiles);
+    const unsigned here = __ballot_sync(0xffffffffu, q.n > 0 && q.agent0 <= a && a < q.agent0 + q.n);
+    if (here && !found) {
+      const int l = __ffs(here) - 1;
+      found = true;
+      mine.agent0 = __shfl_sync(0xffffffffu, q.agent0, l); mine.n = __shfl_sync(0xffffffffu, q.n, l);
+      mine.prefix = __shfl_sync(0xffffffffu, q.prefix, l); mine.steps = __shfl_sync(0xffffffffu, q.steps, l);
+      mine.tiles = __shfl_sync(0xffffffffu, q.tiles, l); mine.cost = __shfl_sync(0xffffffffu, q.cost, l);
+      start = __shfl_sync(0xffffffffu, upto - cost, l);
+      tile0 = __shfl_sync(0xffffffffu, t - q.tiles, l);
+    }
+    total = __shfl_sync(0xffffffffu, upto, 31);
+    tiles = __shfl_sync(0xffffffffu, t, 31);
+  }
+  const int kv = P.kv_lens[a];
+  const bool fine = ascending && found && kv >= 0 && kv <= P.max_kv_len && (kv == 0 || kv >= mine.prefix);
+  if (!fine && lane == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
+  int parts = 0, record = 0, row = 0;                    // of the prefix: parts, the first one's record, the row in it
+  if (fine && kv > 0 && mine.steps > 0) {
+    const Cut cut(total, P.grid);
+    const int i = a - mine.agent0, t = ((i + 1) * mine.tiles - 1) / mine.n, segment = t * heads + head;
+    const int u = start + segment * mine.cost, c = cut.cta_of(u);
+    parts = cut.cta_of(u + mine.steps - 1) - c + 1;
+    record = tile0 * heads + segment + c;
+    row = (i - mine.n * t / mine.tiles) * n_rep + rep;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int kQuads = Dv / 128;
   float4 acc[kQuads];
+  float M = -INFINITY, L = 0.f;
+  bool bad = !fine || kv == 0;
 #pragma unroll
   for (int k = 0; k < kQuads; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  float M = -INFINITY, L = 0.f;
-  bool bad = false;
-  for (int base = 0; base < n_pre + n_own; base += 32) {
-    const int i = base + lane, n = min(32, n_pre + n_own - base);
+  if (!bad && kv > mine.prefix) {                        // the agent's own tokens: a sum that is missing had a bad block in it
+    const float lse = __ldcg(P.own_lse + at);
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) acc[k] = __ldcg(reinterpret_cast<const float4*>(P.own_o + (size_t)at * Dv + 128 * k + 4 * lane));
+    M = lse * kLog2e;
+    L = 1.f;
+    bad = lse == -INFINITY;
+  }
+#pragma unroll 1
+  for (int base = 0; base < parts; base += 32) {
+    const int n = min(32, parts - base);
     float2 ml = make_float2(-INFINITY, 0.f);
-    const float* o = nullptr;
-    if (lane < n) {
-      if (i < n_pre) {
-        ml = __ldcg(P.pre_ml + (size_t)(pre + i) * max_rows + row);
-        o = P.pre_o + (size_t)(pre + i) * record + (size_t)row * Dv;
-      } else {
-        ml = __ldcg(P.suf_ml + (size_t)(own + i - n_pre) * n_rep + rep);
-        o = P.suf_o + ((size_t)(own + i - n_pre) * n_rep + rep) * Dv;
-      }
-    }
+    if (lane < n) ml = __ldcg(P.rec_ml + (size_t)(record + base + lane) * kRows + row);
     bad |= __any_sync(0xffffffffu, ml.y < 0.f) != 0;
-    if (!(ml.y > 0.f) && ml.y == ml.y) ml.x = -INFINITY; // nothing in it
+    const float* o = P.rec_o + ((size_t)(record + base) * kRows + row) * Dv + 4 * lane;
     const float m = fmaxf(M, warp_max(ml.x));
     const float keep = M == -INFINITY ? 0.f : fast_exp2(M - m), e = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
     L = L * keep + warp_sum(e * ml.y);
@@ -837,11 +793,10 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
 #pragma unroll 8
     for (int j = 0; j < n; ++j) {
       const float f = __shfl_sync(0xffffffffu, e, j);
-      const float* from = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), j));
 #pragma unroll
       for (int k = 0; k < kQuads; ++k) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(from + 128 * k + 4 * lane));
-        if (f != 0.f) { acc[k].x = fmaf(f, v.x, acc[k].x); acc[k].y = fmaf(f, v.y, acc[k].y); acc[k].z = fmaf(f, v.z, acc[k].z); acc[k].w = fmaf(f, v.w, acc[k].w); }
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + (size_t)j * kRows * Dv + 128 * k));
+        acc[k].x = fmaf(f, v.x, acc[k].x); acc[k].y = fmaf(f, v.y, acc[k].y); acc[k].z = fmaf(f, v.z, acc[k].z); acc[k].w = fmaf(f, v.w, acc[k].w);
       }
     }
   }
@@ -867,26 +822,41 @@ static_assert(Shape<3, 2>::kRows == Shape<4, 4>::kRows, "");
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The workspace behind the header: the plan, then the records.  A CTA leaves one per segment it touches, and segments and CTAs
-// are both in order, so segment + CTA names a record; tiles: sum over groups of ceil(agents / agents of a tile) at most.
-struct Sections { size_t pre_ml, suf_ml, pre_o, suf_o, end; };
+// The workspace behind the header: the decode launch's records, what it leaves for the agents' own tokens, the prefixes' records (a CTA
+// leaves one per segment it touches).  Tiles: sum over groups of ceil(agents / agents of a tile) at most.
+struct Sections { size_t own_lse, own_o, rec_ml, rec_o, end; };
 Sections sections_of(const Layout& y, int n_agents, int n_groups) {
   const int rows = max_rows_of(y), most = rows / y.n_rep;
-  const size_t tiles = (size_t)n_agents / most + n_groups, n_pre = tiles * y.Hkv + sm_count(), n_suf = (size_t)n_agents * y.Hkv + sm_count();
+  const size_t tiles = (size_t)n_agents / most + n_groups, records = tiles * y.Hkv + sm_count(), q_rows = (size_t)n_agents * y.Hq;
   Sections s;
-  s.pre_ml = align256(sizeof(Plan));
-  s.suf_ml = s.pre_ml + align256(n_pre * rows * sizeof(float2));
-  s.pre_o = s.suf_ml + align256(n_suf * y.n_rep * sizeof(float2));
-  s.suf_o = s.pre_o + align256(n_pre * rows * y.Dv * sizeof(float));
-  s.end = s.suf_o + align256(n_suf * y.n_rep * y.Dv * sizeof(float));
+  s.own_lse = align256(decode_mma_workspace_bytes(y, n_agents));
+  s.own_o = s.own_lse + align256(q_rows * sizeof(float));
+  s.rec_ml = s.own_o + align256(q_rows * y.Dv * sizeof(float));
+  s.rec_o = s.rec_ml + align256(records * rows * sizeof(float2));
+  s.end = s.rec_o + align256(records * rows * y.Dv * sizeof(float));
   return s;
 }
 
+template <class K, class... A>
+cudaError_t launch_pdl(K kernel, int grid, int threads, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <int G, int Gv, bool kBf>
-cudaError_t launch(const Params& P, int grid, cudaStream_t st) {
+cudaError_t launch_prefixes(const Params& P, cudaStream_t st) {
   static bool configured[64] = {};
-  const size_t smem = sizeof(Smem<G, Gv>);
-  static_assert(sizeof(Smem<G, Gv>) <= 227 * 1024, "");
+  constexpr size_t smem = sizeof(Smem<G, Gv>);
+  static_assert(smem <= 227 * 1024, "");
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -895,50 +865,45 @@ cudaError_t launch(const Params& P, int grid, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, shared_prefix_kernel<G, Gv, kBf>, P);
+  return launch_pdl(shared_prefix_kernel<G, Gv, kBf>, P.grid, kThreads, smem, st, P);
+}
+template <int G, int Gv>
+cudaError_t launch_all(const Params& P, const q4kv_batch& b, void* ws, const Sections& s, float scale, cudaStream_t st) {
+  cudaError_t e = P.y.sb_bf16 ? launch_prefixes<G, Gv, true>(P, st) : launch_prefixes<G, Gv, false>(P, st);
   if (e != cudaSuccess) return e;
-  cfg.gridDim = dim3((P.n_agents * P.y.Hq + 3) / 4);
-  cfg.blockDim = dim3(128);
-  cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, shared_prefix_merge_kernel<64 * Gv>, P, (int)Shape<G, Gv>::kRows, (int)Shape<G, Gv>::kRecord);
+  const DecodeGroups groups = {P.group_offs, P.prefix_lens, P.n_groups};
+  const int no_window = 0;
+  e = launch_decode_mma(P.y, P.pool, P.n_blocks, P.layer, b, P.kv_lens, P.max_kv_len, &no_window, 1, P.q, scale, (void*)P.own_o,
+                        Q4KV_OUT_F32, (float*)P.own_lse, ws, P.flags, st, nullptr, nullptr, nullptr, nullptr, &groups);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(shared_prefix_merge_kernel<64 * Gv, Shape<G, Gv>::kRows>, (P.n_agents * P.y.Hq + 3) / 4, 128, 0, st, P);
 }
 
 }  // namespace
 
-bool shared_prefix_supported(const Layout& y, int n_agents, int max_kv_len) {
-  const bool shape = !y.alias && ((y.D == 128 && y.Dv == 128) || (y.D == 256 && y.Dv == 256) || (y.D == 192 && y.Dv == 128));
+bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int max_kv_len) {
   // the list's positions are 32-bit numbers
-  return shape && y.n_rep <= max_rows_of(y) && n_agents <= kMaxAgents &&
-         2ll * n_agents * y.Hkv * (max_kv_len / 128 + 3 + kSegmentCost) < (1ll << 30);
+  return decode_mma_supported(y) && y.n_rep <= max_rows_of(y) && decode_mma_fits(y, n_agents, max_blocks) &&
+         2ll * n_agents * y.Hkv * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
 }
 
 size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups) { return sections_of(y, n_agents, n_groups).end; }
 
+// workspace: with its header (the decode launch's arrival counters)
 cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
                                  int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
-                                 float scale, void* out, int out_dtype, float* lse, void* ws, int32_t* flags, cudaStream_t st) {
+                                 float scale, void* out, int out_dtype, float* lse, void* workspace, int32_t* flags, cudaStream_t st) {
   const Sections s = sections_of(y, b.n_agents, n_groups);
-  uint8_t* at = (uint8_t*)ws;
+  uint8_t* at = (uint8_t*)workspace + kWorkspaceHeaderBytes;
   Params P;
   P.y = y; P.pool = (const uint8_t*)pool; P.n_blocks = n_blocks; P.layer = layer; P.n_agents = b.n_agents; P.max_blocks = b.max_blocks;
   P.tables = b.block_tables; P.kv_lens = kv_lens; P.max_kv_len = max_kv_len; P.group_offs = group_offs; P.prefix_lens = prefix_lens;
-  P.n_groups = n_groups; P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out; P.out_dtype = out_dtype; P.lse = lse;
-  P.flags = flags; P.plan = (Plan*)at; P.pre_ml = (float2*)(at + s.pre_ml); P.suf_ml = (float2*)(at + s.suf_ml);
-  P.pre_o = (float*)(at + s.pre_o); P.suf_o = (float*)(at + s.suf_o);
-  const int grid = sm_count();
-  if (y.D == 128) return y.sb_bf16 ? launch<2, 2, true>(P, grid, st) : launch<2, 2, false>(P, grid, st);
-  if (y.D == 256) return y.sb_bf16 ? launch<4, 4, true>(P, grid, st) : launch<4, 4, false>(P, grid, st);
-  return y.sb_bf16 ? launch<3, 2, true>(P, grid, st) : launch<3, 2, false>(P, grid, st);
+  P.n_groups = n_groups; P.grid = sm_count(); P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out;
+  P.out_dtype = out_dtype; P.lse = lse; P.flags = flags; P.own_lse = (float*)(at + s.own_lse); P.own_o = (float*)(at + s.own_o);
+  P.rec_ml = (float2*)(at + s.rec_ml); P.rec_o = (float*)(at + s.rec_o);
+  if (y.D == 128) return launch_all<2, 2>(P, b, workspace, s, scale, st);
+  if (y.D == 256) return launch_all<4, 4>(P, b, workspace, s, scale, st);
+  return launch_all<3, 2>(P, b, workspace, s, scale, st);
 }
 
 }  // namespace q4kv

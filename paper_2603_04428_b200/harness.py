@@ -86,7 +86,7 @@ class DeviceCache:
         out = torch.empty((A, self.spec.n_q_heads, self.spec.d_v), device="cuda",
                           dtype=torch.float32 if out_dtype == B.OUT_F32 else torch.bfloat16)
         lse = torch.empty((A, self.spec.n_q_heads), dtype=torch.float32, device="cuda") if want_lse else None
-        ws = torch.empty(B.q4kv_workspace_bytes_shared_prefix(self.spec, A, max_kv_len or self.bt.max_blocks * 256, G),
+        ws = torch.zeros(B.q4kv_workspace_bytes_shared_prefix(self.spec, A, max_kv_len or self.bt.max_blocks * 256, G),
                          dtype=torch.uint8, device="cuda")
         B.q4kv_shared_prefix_decode_attention(self.spec, self.pool, self.n_blocks, layer, self.bt, lens_d, max_kv_len, offs_d, pre_d,
                                               G, q, float(scale), out, out_dtype, lse, ws, self.flags)

@@ -298,7 +298,7 @@ def test_the_largest_batch_and_runs_that_repeat():
     with torch.cuda.graph(graph, stream=side):
         for _ in range(3):
             call()
-    ws.fill_(0xFF)
+    ws[B.WORKSPACE_HEADER_BYTES:] = 0xFF
     o2.fill_(9.0)
     graph.replay()
     torch.cuda.synchronize()
@@ -384,12 +384,12 @@ def test_refusals():
     for bad in (dict(sp=make(2, 8, 2, 64, 64)), dict(sp=make(2, 16, 1, 576, 512, True)), dict(sp=make(2, 8, 2, 128, 128, True)),
                 dict(sp=make(2, 130, 2, 128, 128)), dict(sp=make(2, 66, 2, 256, 256)), dict(sp=make(2, 33, 1, 192, 128)),
                 dict(sp=make(2, 8, 2, 128, 128, exact_products=True)), dict(scale=0.0), dict(scale=0.2), dict(scale=-0.1),
-                dict(agents=513), dict(max_blocks=2**23), dict(agents=512, max_blocks=2**22, max_kv=0, sp=make(2, 64, 64, 128, 128))):
+                dict(agents=8193), dict(max_blocks=2**23), dict(agents=512, max_blocks=2**22, max_kv=0, sp=make(2, 64, 64, 128, 128))):
         assert call(**bad) == B.EUNSUPPORTED, bad
     need = B.q4kv_workspace_bytes_shared_prefix(spec, 2, 1024, 1)
     assert need > B.WORKSPACE_HEADER_BYTES and call(size=need - 1) == B.EWORKSPACE
     assert call(agents=0, tables=None) == B.OK
-    for args in ((make(2, 8, 2, 64, 64), 2, 1024, 1), (spec, 513, 1024, 1), (spec, -1, 1024, 1), (spec, 2, -1, 1), (spec, 2, 1024, 3),
+    for args in ((make(2, 8, 2, 64, 64), 2, 1024, 1), (spec, 8193, 1024, 1), (spec, -1, 1024, 1), (spec, 2, -1, 1), (spec, 2, 1024, 3),
                  (spec, 2, 1024, -1)):
         assert B.q4kv_workspace_bytes_shared_prefix(*args) == 0
     assert B.q4kv_workspace_bytes_shared_prefix(spec, 3, 1024, 1) >= need
