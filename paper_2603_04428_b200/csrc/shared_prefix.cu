@@ -8,22 +8,27 @@
 // Three launches: the prefixes (here), the agents' own tokens (decode_mma, its range beginning behind the prefix), the sum of the parts
 // (here).
 //
-// The prefixes' work is a list of segments (group, tile of agents, KV head) with up to kRows score rows each, cut into equal contiguous
+// The prefixes' work is a list of segments (group, tile of score rows, KV head) with up to kRows rows each, cut into equal contiguous
 // ranges of 128-key steps, one per CTA and one CTA per SM; every CTA leaves a record per segment that it touched.  One step is two
 // products on the fifth-generation tensor cores with the KEYS as the 128 rows, so that the number of query rows is the free
-// dimension N (16 .. 64) and few rows cost little:
-//   S^T [128 keys][N] = K^ [128][d_qk] Q^T      K^ (binary16, expanded from the codes) in tensor memory, Q in shared memory
-//   O^T [d_v][N]     += V^T [d_v][128] P^T      V^ and P^T (binary16) in shared memory
-// A lane of tensor memory is a key: a warp that expands keys writes its own lanes (no shared-memory tile, no bank conflicts), and a
-// softmax thread has one key and all rows; the mask is a matter of whole lanes.  The sums l stay in the threads' registers until the
-// segment ends.  What a step costs an SM at d = 128: HBM 790 clocks (18.4 KB), tensor pipe 512 at N = 64.
+// dimension N and few rows cost little.  Both multiply the codes themselves: with x^ = c s + b, one (s, b) per key and 64 elements,
+//   S_g^T [128 keys][N]     = C_g [128][64] Q_g^T         C in tensor memory, Q in shared memory; one accumulator per group g,
+//   score                   = sum_g s_g S_g + b_g (sum of q over the group),
+//   O_g^T [d_v][N]         += C_V^T [d_v][128] (P s_g)^T  C_V and P s_g in shared memory: N columns for each of a tile's two groups,
+//   o                       = O_g of the element's group + sum of p b_g.
+// A nibble masked in place in the low bits of a 16-bit lane is the binary16 subnormal c 2^-24, one nibble up it is 16 c 2^-24 (the 16 is
+// divided out of the other operand): five instructions per eight codes, where the expansion to c s + b takes thirteen.  Scores are
+// exact products with binary32 sums; the probabilities times a scale are rounded once to binary16.  (Expanded keys and values, up to
+// 64 rows a segment: 1400 instructions a scheduler and step at N = 16, 2200 clocks, whatever the rows.)
+// A lane of tensor memory is a key: a softmax thread has one key, its scales and biases in registers, and half of the rows; the mask is
+// a matter of whole lanes.  The sums of p and p b_g stay in the threads' registers until the segment ends.  What a step costs an SM
+// at d = 128: HBM 790 clocks (18.4 KB), tensor pipe 512.
 //   * A warp walks the list and streams raw steps into a ring by bulk copies; two warps stage the query rows of the next segment
 //     (bf16 times a power of two per row into binary16, exact).
-//   * Two sets of four warps expand keys, two expand values (dequant8: one binary16 fma per pair, each value rounded once), a set
-//     every second step: a step is some 300 instructions for a warp, and a warp alone gets one in about seven clocks.
-//   * Two sets of four softmax warps share the rows.  The reference m of a row is the score of the segment's first key; it moves when a
-//     probability would exceed 2^kGrow, which is found by all keys of a set together at the barrier that also ends the set's
-//     stores of P.
+//   * Two sets of four warps unpack keys, two values, a set every second step.
+//   * Two sets of four softmax warps share the rows.  The reference m of a row is kMargin above the maximum over the segment's first
+//     step; it moves when a probability would exceed 2^kGrow, which is found by all keys of a set together at the barrier that also
+//     ends the set's stores of P.
 // All waits are bounded; one that runs out raises Q4KV_FLAG_INTERNAL, lets the copies and the tensor pipe drain and gives the
 // tensor memory back.
 #include "prefill_common.cuh"
@@ -39,23 +44,24 @@ constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 16, kLoadWarp = 24, 
 constexpr int kThreads = 28 * 32;
 constexpr int kRegsSoftmax = 112, kRegsOther = 56;       // of the 72 each thread is launched with
 static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + (kThreads - kSoftmaxWarps * 32) * kRegsOther <= kThreads * 72, "");
-constexpr float kGrow = 14.f;                            // probabilities up to 2^14 (binary16 ends at 65504)
+constexpr float kGrow = 2.5f;                            // p <= 2^2.5: p s stays below 65504 for every scale the quantizer can write (8734)
+constexpr float kMargin = 1.f;
 constexpr int kInfo = 8;                                 // segments that the loader may be ahead of the softmax
 constexpr int kSegmentCost = 1;                          // of a segment beside its steps, in steps
-constexpr uint32_t kColS = 0;                            // tensor-memory columns: S^T 2 x kRows, O^T, K^
 
 template <int G, int Gv>
 struct Shape {
   static constexpr int D = 64 * G, Dv = 64 * Gv;
-  static constexpr int kRows = G == 2 ? 64 : 32;         // score rows of a segment at most
+  static constexpr int kRows = G == 4 ? 16 : 32;         // score rows of a segment at most
   static constexpr int kOffKsb = 16 * D, kOffVc = kOffKsb + 128 * G, kOffVsb = kOffVc + 16 * Dv;
   static constexpr int kChunkBytes = kOffVsb + 128 * Gv, kRawBytes = 4 * kChunkBytes;      // a step: 128 keys
-  static constexpr int kRaw = G == 4 ? 2 : 4;            // raw steps in flight
+  static constexpr int kRaw = G == 4 ? 3 : 4;            // raw steps in flight
   static constexpr int kStagesV = G == 4 ? 1 : 2;
-  static constexpr int kTileV = Dv * 128;                // 64 keys of V^, bytes
-  static constexpr int kQueryBytes = kRows * D * 2, kProbBytes = kRows * 128 * 2;
+  static constexpr int kTileV = Dv * 128;                // the value codes of 64 keys, bytes
+  static constexpr int kQueryBytes = kRows * D * 2, kProbBytes = Gv * kRows * 128 * 2;
   static constexpr int kSboQ = (D / 8) * 128;
-  static constexpr uint32_t kColO = 2 * kRows, kColK = kColO + kRows * (Dv / 128);         // K^: two stages of D / 2 columns
+  // tensor-memory columns: S^T (two steps of G accumulators), O^T (two groups for each 128 elements), codes of the keys (two steps)
+  static constexpr uint32_t kColS = 0, kColO = 2 * G * kRows, kColK = kColO + Gv * kRows;
   static_assert(kColK + D <= 512, "");
   static constexpr int kRecord = kRows * Dv;             // floats of a record's o
 };
@@ -84,8 +90,31 @@ struct Params {
   CodeMasks masks;
 };
 
+// Waits in as few instructions as can be: every role's loop holds several, and the kernel's instructions have to be fetched.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, int use, volatile int* abort_flag) {
+  const uint32_t parity = (uint32_t)use & 1u;
+  if (mbar_test_wait(bar, parity)) return true;
+#pragma unroll 1
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+__device__ __forceinline__ bool spin_for(uint64_t* bar, int use, volatile int* abort_flag) {      // without suspending
+  const uint32_t parity = (uint32_t)use & 1u;
+#pragma unroll 1
+  for (uint32_t i = 0; i < (1u << 26); ++i) {
+    if (mbar_test_wait(bar, parity)) return true;
+    if ((i & 255u) == 255u && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+
 // ---- the work list: positions count steps, and kSegmentCost for each segment ----
-struct Group { int agent0, n, prefix, steps, tiles, cost; };   // cost: of one segment
+struct Group { int agent0, n, prefix, steps, tiles, cost; };   // n: agents; tiles: of score rows; cost: of one segment
 template <int kRows>
 __device__ inline Group group_of(const Params& P, int g, bool* fine = nullptr) {
   Group q = {0, 0, 0, 0, 0, 0};
@@ -98,13 +127,14 @@ __device__ inline Group group_of(const Params& P, int g, bool* fine = nullptr) {
       q.n = hi - lo;
       q.prefix = prefix;
       q.steps = (prefix + 127) >> 7;
-      const int most = kRows / P.y.n_rep;
-      q.tiles = (q.n + most - 1) / most;                 // as equal as can be: tile t has agents n t / tiles .. n (t + 1) / tiles - 1
+      q.tiles = (q.n * P.y.n_rep + kRows - 1) / kRows;   // as equal as can be: see tile_begin
       q.cost = q.tiles > 0 && q.steps > 0 ? q.steps + kSegmentCost : 0;
     }
   }
   return q;
 }
+// Score row r of a group and KV head is of the group's agent r / n_rep and that agent's query head r % n_rep; tile t of them begins at
+__device__ inline int tile_begin(int rows, int tiles, int t) { return (int)((long long)rows * t / tiles); }
 __device__ inline int inclusive_sum(int v) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -124,7 +154,7 @@ struct Cut {
 
 // One CTA's part of a segment.  Records are named segment + CTA: both are in order, so no two parts share one.
 struct Segment {
-  int agent0, rows, lead, head;                          // rows: agents agent0 .. x n_rep heads of KV head `head`; keys: of agent `lead`
+  int agent0, row0, rows, lead, head;                    // rows row0 .. of the group that begins with agent0; keys: of agent `lead`
   int prefix, step0, steps;                              // keys of the prefix; 128-key steps of this CTA (0: there is no more)
   int record;
 };
@@ -135,10 +165,11 @@ struct Smem {
   alignas(128) uint8_t vhat[Sh::kStagesV][2 * Sh::kTileV];     // [half][dim][key 64]: (n%8)*16 + (n/8)*1024 + (k/8)*128
   alignas(128) uint8_t raw[Sh::kRaw][Sh::kRawBytes];
   alignas(128) uint8_t qs[2][Sh::kQueryBytes];                 // [row][dim]: (r%8)*16 + (r/8)*kSboQ + (k/8)*128
-  alignas(128) uint8_t prob[2][Sh::kProbBytes];                // [key][row]: (k%8)*16 + (k/8)*128 + (r/8)*2048 + (r%8)*2
-  alignas(16) float kappa[2][Sh::kRows];                       // score in log2 units = S * kappa
-  // of the two softmax sets: minus the reference of each row, what to scale by when it moves, partial maxima and sums
-  alignas(16) float neg_ref[2][Sh::kRows / 2], factor[2][Sh::kRows / 2], red_max[2][4][Sh::kRows / 2], red_sum[2][4][Sh::kRows / 2];
+  alignas(128) uint8_t prob[2][Sh::kProbBytes];                // [key][value group x rows, row]: (k%8)*16 + (k/8)*128 + (r/8)*2048 + (r%8)*2
+  // of a row: what S_g times the scale is multiplied by for a score in log2 units, and the sums of q over the groups in those
+  alignas(16) float kappa[2][Sh::kRows], q_sum[2][G][Sh::kRows];
+  // of the two softmax sets: minus the reference of each row, what to scale by when it moves, partial maxima, sums of p and p b_g
+  alignas(16) float neg_ref[2][Sh::kRows / 2], factor[2][Sh::kRows / 2], red_max[2][4][Sh::kRows / 2], red_sum[2][4][Gv + 1][Sh::kRows / 2];
   alignas(8) uint64_t raw_full[Sh::kRaw], raw_free[Sh::kRaw];
   uint64_t k_full[2], s_full[2], p_full[2], o_done[2], q_full[2], q_free[2], info_full[kInfo], info_free[kInfo], drain;
   Segment info[kInfo];
@@ -168,9 +199,10 @@ __device__ inline float warp_sum(float v) {
 template <int kCount>
 __device__ inline float column_sums(float (&v)[kCount]) {
   const int lane = threadIdx.x & 31;
-  if (kCount == 16) {
 #pragma unroll
-    for (int c = 0; c < kCount; ++c) v[c] += __shfl_xor_sync(0xffffffffu, v[c], 16);
+  for (int o = 16; o >= kCount; o >>= 1) {
+#pragma unroll
+    for (int c = 0; c < kCount; ++c) v[c] += __shfl_xor_sync(0xffffffffu, v[c], o);
   }
 #pragma unroll
   for (int o = kCount / 2; o > 0; o >>= 1) {
@@ -179,6 +211,29 @@ __device__ inline float column_sums(float (&v)[kCount]) {
     for (int c = 0; c < o; ++c) v[c] = (high ? v[c + o] : v[c]) + __shfl_xor_sync(0xffffffffu, high ? v[c] : v[c + o], o);
   }
   return v[0];
+}
+
+// query8 with the elements that meet a nibble's second place divided by 16
+__device__ inline uint4 query_codes8(uint4 v, float sf) {
+  const float sh = sf * 0.0625f;
+  auto lo = [](uint32_t u) { return __uint_as_float(u << 16); };
+  auto hi = [](uint32_t u) { return __uint_as_float(u & 0xffff0000u); };
+  return make_uint4(f32x2_to_h2(lo(v.x) * sf, lo(v.z) * sf), f32x2_to_h2(hi(v.x) * sh, hi(v.z) * sh), f32x2_to_h2(lo(v.y) * sf, lo(v.w) * sf),
+                    f32x2_to_h2(hi(v.y) * sh, hi(v.w) * sh));
+}
+__device__ inline float sum_of8(uint4 v) {
+  auto two = [](uint32_t u) { return __uint_as_float(u << 16) + __uint_as_float(u & 0xffff0000u); };
+  return (two(v.x) + two(v.y)) + (two(v.z) + two(v.w));
+}
+// Eight codes as binary16 subnormals, in the order 0,4,1,5,2,6,3,7: c 2^-24 and (1,5,3,7) 16 c 2^-24
+__device__ inline uint4 codes8(uint32_t w, const CodeMasks& m) {
+  const uint32_t wh = w >> 8;
+  return make_uint4(w & m.lo, w & m.hi, wh & m.lo, wh & m.hi);
+}
+template <bool kBf>
+__device__ inline float2 scale_bias(uint32_t u) {
+  if (kBf) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
 }
 
 template <int G, int Gv, bool kBf>
@@ -192,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kRaw; ++s) { mbar_init(&sm.raw_full[s], 1); mbar_init(&sm.raw_free[s], 8); sm.bad[s] = 0; }
+    for (int s = 0; s < kRaw; ++s) { mbar_init(&sm.raw_full[s], 1); mbar_init(&sm.raw_free[s], 16); sm.bad[s] = 0; }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&sm.k_full[s], 4); mbar_init(&sm.s_full[s], 1); mbar_init(&sm.p_full[s], 6); mbar_init(&sm.o_done[s], 1);
       mbar_init(&sm.q_full[s], 64); mbar_init(&sm.q_free[s], 3);
@@ -248,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       int n = 0;                                         // segments handed out
       bool ok = true;
       auto hand_out = [&](const Segment& s) {
-        if (n >= kInfo && !mbar_wait(&sm.info_free[n % kInfo], (uint32_t)(n / kInfo - 1), abort_flag)) ok = false;
+        if (n >= kInfo && !wait_for(&sm.info_free[n % kInfo], n / kInfo - 1, abort_flag)) ok = false;
         if (ok && lane == 0) {
           sm.info[n % kInfo] = s;
           sm.poisoned[n % kInfo] = 0;
@@ -274,16 +329,18 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           if (at >= u1) break;
           const int from = max(0, u0 - at), to = min(q.steps, u1 - at);
           if (from >= to) continue;                      // this CTA's part is the segment's fixed cost
-          const int t = k / y.Hkv, a = q.n * t / q.tiles;
+          const int t = k / y.Hkv, all = q.n * y.n_rep;
           Segment s;
-          s.agent0 = q.agent0 + a; s.rows = (q.n * (t + 1) / q.tiles - a) * y.n_rep; s.lead = lead; s.head = k - t * y.Hkv;
+          s.agent0 = q.agent0; s.row0 = tile_begin(all, q.tiles, t); s.rows = tile_begin(all, q.tiles, t + 1) - s.row0;
+          s.lead = lead; s.head = k - t * y.Hkv;
           s.prefix = q.prefix; s.step0 = from; s.steps = to - from; s.record = tile0 * y.Hkv + k + (int)blockIdx.x;
           hand_out(s);
           if (lane == 0) {
             const uint8_t* row = head_block(P.pool, y, P.layer, 0, s.head);
+#pragma unroll 1
             for (int j = 0; ok && j < s.steps; ++j, ++g) {
               const int r = g % kRaw, step = s.step0 + j;
-              if (g >= kRaw && !mbar_wait(&sm.raw_free[r], (uint32_t)(g / kRaw - 1), abort_flag)) { ok = false; break; }
+              if (g >= kRaw && !wait_for(&sm.raw_free[r], g / kRaw - 1, abort_flag)) { ok = false; break; }
               const int blk = P.tables[(size_t)s.lead * P.max_blocks + (step >> 1)];
               sm.bad[r] = blk < 0 || blk >= P.n_blocks;
               if (sm.bad[r]) {
@@ -306,21 +363,24 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       hand_out(last);
       // a CTA that is giving up still lets its own copies land before shared memory is released
       if (lane == 0 && *abort_flag)
+#pragma unroll 1
         for (int j = max(0, g - kRaw); j < g; ++j)
+#pragma unroll 1
           for (uint32_t i = 0; i < kSpinLimit && !mbar_try_wait(&sm.raw_full[j % kRaw], (uint32_t)(j / kRaw) & 1u); ++i) {}
     } else if (warp == kMmaWarp) {
       // =============================== products ===================================================
       // A product's commit also covers what was issued before it: S^T of a step implies O^T of the step two before, so neither the
       // buffers of P^T nor those of S^T and K^ need barriers of their own.  The value tile's warps arrive where the softmax does.
       auto wait = [&](uint64_t* bar, int use) {
-        const bool ok = mbar_spin(bar, (uint32_t)use, abort_flag);
+        const bool ok = spin_for(bar, use, abort_flag);
         if (ok) fence_after_sync();
         return ok;
       };
       const uint64_t vd0 = smem_desc(smem_u32(sm.vhat[0]), 128, 1024), pd0 = smem_desc(smem_u32(sm.prob[0]), 128, 2048);
       const uint64_t qd0 = smem_desc(smem_u32(sm.qs[0]), 128, Sh::kSboQ);
       bool first = true;
-      uint32_t idesc_pv = 0;                             // of the step whose value product is due
+      uint32_t idesc_pv = 0;                             // of the step whose value product is due, and its two groups of P s_g
+      int p_tile = 0;
       auto issue_pv = [&](int h) {                       // O^T (+)= V^T P^T of step h
         const uint64_t vd = vd0 + (uint64_t)((h % kStagesV) * (2 * Sh::kTileV >> 4)), pd = pd0 + (uint64_t)((h & 1) * (Sh::kProbBytes >> 4));
         if (elect_one()) {
@@ -328,27 +388,30 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           for (int m = 0; m < Dv / 128; ++m)
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              mma_f16_ss(tb + Sh::kColO + kRows * m, vd + (uint64_t)((k >> 2) * (Sh::kTileV >> 4) + m * 1024 + (k & 3) * 16), pd + 16 * k, idesc_pv,
-                         (!first || k > 0) ? 1u : 0u);
+              mma_f16_ss(tb + Sh::kColO + 2 * kRows * m, vd + (uint64_t)((k >> 2) * (Sh::kTileV >> 4) + m * 1024 + (k & 3) * 16),
+                         pd + (uint64_t)(m * p_tile + 16 * k), idesc_pv, (!first || k > 0) ? 1u : 0u);
           commit(&sm.o_done[h & 1]);
         }
         __syncwarp();
       };
       bool ok = true;
+#pragma unroll 1
       for (int n = 0; ok; ++n) {
         const int slot = n & 1;
         ok = wait(&sm.q_full[slot], n >> 1);
         const int steps = ok ? sm.info[n % kInfo].steps : 0, columns = ok ? (sm.info[n % kInfo].rows + 15) & ~15 : 0;
         const uint32_t size = (uint32_t)(columns >> 3) << 17;
         const uint64_t qd = qd0 + (uint64_t)(slot * (Sh::kQueryBytes >> 4));
+#pragma unroll 1
         for (int j = 0; ok && (j < steps || (steps == 0 && j == 0)); ++j) {
           if (steps > 0) {
             ok = wait(&sm.k_full[g & 1], g >> 1);
             if (!ok) break;
             if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < D / 16; ++k)
-                mma_f16_ts(tb + kColS + kRows * (g & 1), tb + Sh::kColK + (D / 2) * (g & 1) + 8 * k, qd + 16 * k, idesc_f16(128, 0) | size, k > 0);
+              for (int k = 0; k < D / 16; ++k)           // four products for each group's accumulator
+                mma_f16_ts(tb + Sh::kColS + kRows * (G * (g & 1) + (k >> 2)), tb + Sh::kColK + (D / 2) * (g & 1) + 8 * k, qd + 16 * k,
+                           idesc_f16(128, 0) | size, (k & 3) > 0);
               commit(&sm.s_full[g & 1]);
               if (j == steps - 1) commit(&sm.q_free[slot]);
             }
@@ -359,7 +422,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             if (ok) issue_pv(g - 1);
           }
           first = j == 0;
-          idesc_pv = idesc_f16(128, 0, 0, 1) | size;
+          idesc_pv = idesc_f16(128, 0, 0, 1) | (size << 1);
+          p_tile = (columns >> 3) * (2 * 2048 >> 4);
           ++g;
         }
         if (steps == 0) break;
@@ -369,20 +433,23 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       constexpr int kLanes = D == 128 ? 16 : 32, kAtOnce = 4, kStride = 2 * (32 / kLanes);     // lanes of a row, rows in flight, rows of both warps
       asm volatile("griddepcontrol.wait;" ::: "memory");
       const int piece = lane % kLanes, sub = (warp - kQueryWarp) * (32 / kLanes) + lane / kLanes;
+#pragma unroll 1
       for (int n = 0;; ++n) {
         const int slot = n & 1;
-        if (!mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag)) break;
+        if (!wait_for(&sm.info_full[n % kInfo], n / kInfo, abort_flag)) break;
         const Segment& s = sm.info[n % kInfo];
         const int steps = s.steps, rows = s.rows, padded = steps > 0 ? (rows + 15) & ~15 : 0;
+        const int row0 = s.row0;
         const uint16_t* q = P.q + ((size_t)s.agent0 * y.Hq + (size_t)s.head * y.n_rep) * D + 8 * piece;
-        if (n >= 2 && !mbar_wait(&sm.q_free[slot], (uint32_t)((n >> 1) - 1), abort_flag)) break;
+        if (n >= 2 && !wait_for(&sm.q_free[slot], (n >> 1) - 1, abort_flag)) break;
+#pragma unroll 1
         for (int base = sub; base < padded; base += kStride * kAtOnce) {
           uint4 v[kAtOnce];
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
-            const int r = base + kStride * u, a = r / y.n_rep;
+            const int r = base + kStride * u, a = (row0 + r) / y.n_rep;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows && piece < D / 8) v[u] = *reinterpret_cast<const uint4*>(q + ((size_t)a * y.Hq + (r - a * y.n_rep)) * D);
+            if (r < rows && piece < D / 8) v[u] = *reinterpret_cast<const uint4*>(q + ((size_t)a * y.Hq + (row0 + r - a * y.n_rep)) * D);
           }
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
@@ -394,9 +461,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             if (mx == 0.f) ex = 0;
             ex = min(max(ex, -100), 100);
             const float sf = __uint_as_float((uint32_t)(127 + 8 - ex) << 23);          // 256 <= max |q| * sf < 512
+            float sum = sum_of8(v[u]);
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o, kLanes);       // over the eight pieces of a group
             if (r < padded) {
-              if (piece == 0) sm.kappa[slot][r] = P.scale_log2 * __uint_as_float((uint32_t)(127 - 8 + ex) << 23);
-              if (piece < D / 8) *reinterpret_cast<uint4*>(sm.qs[slot] + (r & 7) * 16 + (r >> 3) * Sh::kSboQ + piece * 128) = query8(v[u], sf);
+              if (piece == 0) sm.kappa[slot][r] = P.scale_log2 * __uint_as_float((uint32_t)(127 - 8 + 24 + ex) << 23);
+              if ((piece & 7) == 0 && piece < D / 8) sm.q_sum[slot][piece >> 3][r] = P.scale_log2 * sum;
+              if (piece < D / 8) *reinterpret_cast<uint4*>(sm.qs[slot] + (r & 7) * 16 + (r >> 3) * Sh::kSboQ + piece * 128) = query_codes8(v[u], sf);
             }
           }
         }
@@ -412,49 +483,33 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     // one 16-byte piece (dims 32 vq + 8 k + vr, k = 0..3) of token octet vo of a chunk; at d_v = 256 vq + 4 as well
     const int vr = x7 & 7, vq = (x7 >> 3) & 3, vo = ((vr >> 1) + (x7 >> 5)) & 3;
     const int v_read = Sh::kOffVc + ((vq * 8 + vr) * 4 + vo) * 16, v_write = vr * 16 + (4 * vq) * 1024 + vo * 128;
-    const int v_sb = Sh::kOffVsb + (vo * 2 * Gv + (vq >> 1)) * 4;           // + (i * 8 + e) * Gv * 4: token 8 vo + 4 e + i
-    for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
-      const int key1 = sm.info[n % kInfo].prefix, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+#pragma unroll 1
+    for (int n = 0; wait_for(&sm.info_full[n % kInfo], n / kInfo, abort_flag); ++n) {
+      const int steps = sm.info[n % kInfo].steps;
       bool go = steps > 0;
+#pragma unroll 1
       for (int j = 0; go && j < steps; ++j, ++g) {
         if ((g & 1) != mine) continue;
         const int r = g % kRaw, sv = g % kStagesV;
-        go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
-             (g < kStagesV || mbar_wait(&sm.o_done[(g - kStagesV) & 1], (uint32_t)((g - kStagesV) >> 1), abort_flag));
+        go = wait_for(&sm.raw_full[r], g / kRaw, abort_flag) &&
+             (g < kStagesV || wait_for(&sm.o_done[(g - kStagesV) & 1], (g - kStagesV) >> 1, abort_flag));
         if (!go) break;
-        const bool bad = sm.bad[r] != 0;
-        bool over = false;
-#pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          const uint8_t* chunk = sm.raw[r] + c * Sh::kChunkBytes;
-          const int at = (step0 + j) * 128 + c * 32, pos = at + 8 * vo;
-          const bool edge = bad || at + 32 > key1;       // some of its bytes are none of the prefix's
 #pragma unroll
-          for (int half = 0; half < Gv / 2; ++half) {
-            const uint4 vw = *reinterpret_cast<const uint4*>(chunk + v_read + half * (4 * 8 * 4 * 16));
-            uint32_t e[8];
+        for (int half = 0; half < Gv / 2; ++half) {
+          const uint8_t* from = sm.raw[r] + v_read + half * (4 * 8 * 4 * 16);
+          uint8_t* dst = sm.vhat[sv] + v_write + half * 16384;
+          uint4 w[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = *reinterpret_cast<const uint32_t*>(chunk + v_sb + half * 8 + ((i & 3) * 8 + (i >> 2)) * Gv * 4);
-            if (edge) {
+          for (int c = 0; c < 4; ++c) w[c] = *reinterpret_cast<const uint4*>(from + c * Sh::kChunkBytes);
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (bad || pos + i >= key1) e[i] = 0u;
-            }
-            uint32_t sp[4], bp[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (kBf) { e[i] = bf16_pair_to_h2(e[i], over); e[i + 4] = bf16_pair_to_h2(e[i + 4], over); }
-              sp[i] = __byte_perm(e[i], e[i + 4], 0x5410);
-              bp[i] = __byte_perm(e[i], e[i + 4], 0x7632);
-            }
-            uint8_t* dst = sm.vhat[sv] + v_write + (c >> 1) * Sh::kTileV + (c & 1) * 512 + half * 16384;
-            *reinterpret_cast<uint4*>(dst + 0 * 1024) = dequant8(vw.x, sp[0], bp[0], sp[1], bp[1], sp[2], bp[2], sp[3], bp[3], P.masks);
-            *reinterpret_cast<uint4*>(dst + 1 * 1024) = dequant8(vw.y, sp[0], bp[0], sp[1], bp[1], sp[2], bp[2], sp[3], bp[3], P.masks);
-            *reinterpret_cast<uint4*>(dst + 2 * 1024) = dequant8(vw.z, sp[0], bp[0], sp[1], bp[1], sp[2], bp[2], sp[3], bp[3], P.masks);
-            *reinterpret_cast<uint4*>(dst + 3 * 1024) = dequant8(vw.w, sp[0], bp[0], sp[1], bp[1], sp[2], bp[2], sp[3], bp[3], P.masks);
+          for (int c = 0; c < 4; ++c) {
+            uint8_t* to = dst + (c >> 1) * Sh::kTileV + (c & 1) * 512;
+            *reinterpret_cast<uint4*>(to + 0 * 1024) = codes8(w[c].x, P.masks);
+            *reinterpret_cast<uint4*>(to + 1 * 1024) = codes8(w[c].y, P.masks);
+            *reinterpret_cast<uint4*>(to + 2 * 1024) = codes8(w[c].z, P.masks);
+            *reinterpret_cast<uint4*>(to + 3 * 1024) = codes8(w[c].w, P.masks);
           }
         }
-        if (kBf && over) raise_flag(P.flags, Q4KV_FLAG_SB_RANGE);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) { mbar_arrive(&sm.p_full[g & 1]); mbar_arrive(&sm.raw_free[r]); }
@@ -468,41 +523,31 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     // words 16 j + 4 m + t lie in four 16-byte pieces t; lane l begins with piece l / 2 % 4 (no bank conflicts) and turns them back.
     const int c = warp & 3, mine = (warp - kKeyWarp) >> 2, tau = 8 * (lane >> 3) + elem_of(lane & 7), ti = tau & 3, tg = tau >> 2, rot = (lane >> 1) & 3;
     const int k_read = c * Sh::kChunkBytes + ti * (256 * G) + tg * 64;      // + j * 512 + piece * 16
-    const int k_sb = c * Sh::kChunkBytes + Sh::kOffKsb + ((ti * 4 + (tau >> 3)) * 2 + ((tau >> 2) & 1)) * G * 4;
     const uint32_t lane_addr = tb + ((uint32_t)(c * 32) << 16) + Sh::kColK;
     auto turned = [&](uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t* out) {      // out[t] = what came as number (t - rot) & 3
       const bool one = rot & 1, two = rot & 2;
       const uint32_t b0 = one ? a3 : a0, b1 = one ? a0 : a1, b2 = one ? a1 : a2, b3 = one ? a2 : a3;
       out[0] = two ? b2 : b0; out[1] = two ? b3 : b1; out[2] = two ? b0 : b2; out[3] = two ? b1 : b3;
     };
-    for (int n = 0; mbar_wait(&sm.info_full[n % kInfo], (uint32_t)(n / kInfo), abort_flag); ++n) {
-      const int key1 = sm.info[n % kInfo].prefix, step0 = sm.info[n % kInfo].step0, steps = sm.info[n % kInfo].steps;
+#pragma unroll 1
+    for (int n = 0; wait_for(&sm.info_full[n % kInfo], n / kInfo, abort_flag); ++n) {
+      const int steps = sm.info[n % kInfo].steps;
       bool go = steps > 0;
+#pragma unroll 1
       for (int j = 0; go && j < steps; ++j, ++g) {
         if ((g & 1) != mine) continue;
         const int r = g % kRaw;
-        go = mbar_wait(&sm.raw_full[r], (uint32_t)(g / kRaw), abort_flag) &&
-             (g < 2 || mbar_wait(&sm.s_full[g & 1], (uint32_t)((g >> 1) - 1), abort_flag));
+        go = wait_for(&sm.raw_full[r], g / kRaw, abort_flag) &&
+             (g < 2 || wait_for(&sm.s_full[g & 1], (g >> 1) - 1, abort_flag));
         if (!go) break;
         fence_after_sync();
-        const int pos = (step0 + j) * 128 + c * 32 + tau;
-        const bool none = sm.bad[r] != 0 || pos >= key1;
         const uint8_t* raw = sm.raw[r];
-        uint32_t sb[G];
-        bool over = false;
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-          sb[i] = none ? 0u : *reinterpret_cast<const uint32_t*>(raw + k_sb + 4 * i);
-          if (kBf) sb[i] = bf16_pair_to_h2(sb[i], over);
-        }
-        if (kBf && over) raise_flag(P.flags, Q4KV_FLAG_SB_RANGE);
         const uint32_t to = lane_addr + (D / 2) * (g & 1);
-        auto expand = [&](const uint32_t* words, uint32_t e, uint32_t at) {          // four words of one group: 16 columns
-          const uint32_t s2 = __byte_perm(e, e, 0x1010), b2 = __byte_perm(e, e, 0x3232);
+        auto expand = [&](const uint32_t* words, uint32_t at) {              // four words: 16 columns
           uint32_t col[16];
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            const uint4 v = dequant8(words[t], s2, b2, P.masks);
+            const uint4 v = codes8(words[t], P.masks);
             col[4 * t] = v.x; col[4 * t + 1] = v.y; col[4 * t + 2] = v.z; col[4 * t + 3] = v.w;
           }
           tmem_st16(to + at, col);
@@ -514,8 +559,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
 #pragma unroll
             for (int t = 0; t < 4; ++t) p[t] = *reinterpret_cast<const uint2*>(raw + k_read + (jj >> 1) * 512 + (jj & 1) * 8 + ((t + rot) & 3) * 16);
             uint32_t wd[4];
-            turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, sb[jj], 32 * jj);
-            turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, sb[jj], 32 * jj + 16);
+            turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, 32 * jj);
+            turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, 32 * jj + 16);
           }
         }
         if (G & 1) {                                     // the last group: 8-byte pieces, words 16 + 4 m + t, m = 0, 1
@@ -524,8 +569,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
 #pragma unroll
           for (int t = 0; t < 4; ++t) p[t] = *reinterpret_cast<const uint2*>(raw + at + ((t + rot) & 3) * 8);
           uint32_t wd[4];
-          turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, sb[G - 1], 32 * (G - 1));
-          turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, sb[G - 1], 32 * (G - 1) + 16);
+          turned(p[0].x, p[1].x, p[2].x, p[3].x, wd); expand(wd, 32 * (G - 1));
+          turned(p[0].y, p[1].y, p[2].y, p[3].y, wd); expand(wd, 32 * (G - 1) + 16);
         }
         wait_st();
         fence_before_sync();
@@ -540,114 +585,148 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     // (inside a segment no thread leaves early: after an abort every wait returns at once, and the barriers stay even)
     const int set = warp >> 2, quad = warp & 3;
     const uint32_t lane_addr = tb + ((uint32_t)(quad * 32) << 16);
-    const int key = quad * 32 + 8 * (lane >> 3) + elem_of(lane & 7);       // of the step
+    const int tau = 8 * (lane >> 3) + elem_of(lane & 7), key = quad * 32 + tau;            // in the chunk, of the step
+    const int at_sb = (((tau & 3) * 4 + (tau >> 3)) * 2 + ((tau >> 2) & 1)) * 4;             // of a token's (scale, bias) words, times groups
+    const float place = tau & 1 ? 0.0625f : 1.f;                             // its value codes' place in their 16-bit lanes
     const int tid = threadIdx.x & 127;
     float* const neg_ref = sm.neg_ref[set];
     float* const factor = sm.factor[set];
+#pragma unroll 1
     for (int n = 0;; ++n) {
       const int slot = n & 1;
       bool lost = false;
-      if (quad == set) lost = !mbar_spin(&sm.q_full[slot], (uint32_t)(n >> 1), abort_flag);
+      if (quad == set) lost = !spin_for(&sm.q_full[slot], n >> 1, abort_flag);
       if (set_any(set, lost)) break;
       const Segment s = sm.info[n % kInfo];
       if (s.steps == 0) break;
-      const int rows = s.rows, first = set * (((rows + 15) & ~15) >> 1);
-      const int mine = min(max((rows - first + 7) >> 3, 0), ((rows + 15) & ~15) >> 4);       // groups of eight rows, from row `first` on
-      const float* kap = sm.kappa[slot] + first;
-      uint64_t l[4 * kGroups];
+      const int half = ((s.rows + 15) & ~15) >> 1, first = set * half;
+      const int mine = min(max((s.rows - first + 7) >> 3, 0), half >> 3);    // groups of eight rows, from row `first` on
+      uint64_t l[4 * kGroups], pb[Gv][4 * kGroups];      // sums of p and p b_g
 #pragma unroll
-      for (int c = 0; c < 4 * kGroups; ++c) l[c] = 0ull;
+      for (int c = 0; c < 4 * kGroups; ++c) {
+        l[c] = 0ull;
+#pragma unroll
+        for (int v = 0; v < Gv; ++v) pb[v][c] = 0ull;
+      }
+      bool started = false;
 #pragma unroll 1
       for (int j = 0; j < s.steps; ++j, ++g) {
-        const int b = g & 1;
-        mbar_wait(&sm.s_full[b], (uint32_t)(g >> 1), abort_flag);
+        const int b = g & 1, r = g % kRaw;
+        wait_for(&sm.s_full[b], g >> 1, abort_flag);
         fence_after_sync();
         const bool edge = (s.step0 + j) * 128 + 128 > s.prefix, valid = (s.step0 + j) * 128 + key < s.prefix;
-        const uint32_t s_addr = lane_addr + kColS + kRows * b + first;
-        uint8_t* const p_at = sm.prob[b] + (quad * 32 + lane) * 16 + (first >> 3) * 2048;
-        if (j == 0) {                                    // a first reference for every row: the score of the first key
-          if (quad == 0) {
-#pragma unroll 1
-            for (int i = 0; i < mine; ++i) {
-              uint32_t x[8];
-              tmem_ld8(s_addr + 8 * i, x);
-              wait_ld8(x);
-              if (lane == 0) {
+        wait_for(&sm.raw_full[r], g / kRaw, abort_flag);
+        // the key's scales and biases
+        uint64_t ks[G], kb[G], vs[Gv], vb[Gv];
+        {
+          const uint8_t* chunk = sm.raw[r] + quad * Sh::kChunkBytes;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) neg_ref[8 * i + c] = -(__uint_as_float(x[c]) * kap[8 * i + c]);
-              }
-            }
+          for (int i = 0; i < G; ++i) {
+            const float2 e = scale_bias<kBf>(*reinterpret_cast<const uint32_t*>(chunk + Sh::kOffKsb + at_sb * G + 4 * i));
+            ks[i] = pair64(e.x, e.x);
+            kb[i] = pair64(e.y, e.y);
           }
-          set_sync(set);
+#pragma unroll
+          for (int i = 0; i < Gv; ++i) {
+            float2 e = scale_bias<kBf>(*reinterpret_cast<const uint32_t*>(chunk + Sh::kOffVsb + at_sb * Gv + 4 * i));
+            if (edge && !valid) e = make_float2(0.f, 0.f);
+            vs[i] = pair64(e.x * place, e.x * place);
+            vb[i] = pair64(e.y, e.y);
+          }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.raw_free[r]);
+        const uint32_t s_addr = lane_addr + Sh::kColS + kRows * G * b + first;
         uint64_t p[4 * kGroups];
+        // scores of eight rows, in log2 units above their references
+        auto scores = [&](int i, uint64_t (&t)[4], bool relative) {
+          uint32_t x[G][8];
+#pragma unroll
+          for (int v = 0; v < G; ++v) tmem_ld8(s_addr + kRows * v + 8 * i, x[v]);
+#pragma unroll
+          for (int v = 0; v < G; ++v) wait_ld8(x[v]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int row = first + 8 * i + 2 * c;
+            uint64_t w = relative ? *reinterpret_cast<const uint64_t*>(neg_ref + 8 * i + 2 * c) : 0ull;
+            uint64_t u = mul2(pair64(__uint_as_float(x[0][2 * c]), __uint_as_float(x[0][2 * c + 1])), ks[0]);
+#pragma unroll
+            for (int v = 1; v < G; ++v) u = fma2(pair64(__uint_as_float(x[v][2 * c]), __uint_as_float(x[v][2 * c + 1])), ks[v], u);
+#pragma unroll
+            for (int v = 0; v < G; ++v) w = fma2(*reinterpret_cast<const uint64_t*>(&sm.q_sum[slot][v][row]), kb[v], w);
+            t[c] = fma2(u, *reinterpret_cast<const uint64_t*>(&sm.kappa[slot][row]), w);
+          }
+        };
         bool grown = false;
 #pragma unroll 1
         for (;;) {
-          uint32_t x[8 * kGroups];
-          float most = -INFINITY;
+          if (started) {
+            float most = -INFINITY;
+            uint8_t* const p_at = sm.prob[b] + (quad * 32 + lane) * 16 + (first >> 3) * 2048;
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i)
-            if (i < mine) tmem_ld8(s_addr + 8 * i, x + 8 * i);
-          if (kGroups == 4) wait_ld32(x); else wait_ld16(x);
-          if (edge && !valid) {
+            for (int i = 0; i < kGroups; ++i) {
+              if (i < mine) {
+                uint64_t t[4];
+                scores(i, t, true);
 #pragma unroll
-            for (int c = 0; c < 8 * kGroups; ++c) x[c] = 0xff800000u;
-          }
+                for (int c = 0; c < 4; ++c) {
+                  const float2 e = unpair64(t[c]);
+                  if (!edge || valid) most = fmaxf(fmaxf(most, e.x), e.y);
+                  p[4 * i + c] = edge && !valid ? 0ull : pair64(fast_exp2(e.x), fast_exp2(e.y));
+                }
 #pragma unroll
-          for (int i = 0; i < kGroups; ++i) {
-            if (i < mine) {
-              uint32_t h[4];
+                for (int v = 0; v < Gv; ++v) {
+                  uint32_t h[4];
 #pragma unroll
-              for (int c = 0; c < 4; c += 2) {
-                const ulonglong2 kk = *reinterpret_cast<const ulonglong2*>(kap + 8 * i + 2 * c), rr = *reinterpret_cast<const ulonglong2*>(neg_ref + 8 * i + 2 * c);
-                const float2 t0 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c]), __uint_as_float(x[8 * i + 2 * c + 1])), kk.x, rr.x));
-                const float2 t1 = unpair64(fma2(pair64(__uint_as_float(x[8 * i + 2 * c + 2]), __uint_as_float(x[8 * i + 2 * c + 3])), kk.y, rr.y));
-                most = fmaxf(fmaxf(most, t0.x), t0.y);
-                most = fmaxf(fmaxf(most, t1.x), t1.y);
-                const float a0 = fast_exp2(t0.x), a1 = fast_exp2(t0.y), b0 = fast_exp2(t1.x), b1 = fast_exp2(t1.y);
-                p[4 * i + c] = pair64(a0, a1);
-                p[4 * i + c + 1] = pair64(b0, b1);
-                h[c] = f32x2_to_h2(a0, a1);
-                h[c + 1] = f32x2_to_h2(b0, b1);
+                  for (int c = 0; c < 4; ++c) { const float2 e = unpair64(mul2(p[4 * i + c], vs[v])); h[c] = f32x2_to_h2(e.x, e.y); }
+                  *reinterpret_cast<uint4*>(p_at + i * 2048 + v * (half >> 2) * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
+                }
               }
-              *reinterpret_cast<uint4*>(p_at + i * 2048) = make_uint4(h[0], h[1], h[2], h[3]);
             }
+            fence_async_smem();
+            fence_before_sync();
+            if (!set_any(set, most > kGrow) || grown) break;
+            fence_after_sync();
+          } else if (mine == 0) {
+            break;
           }
-          fence_async_smem();
-          fence_before_sync();
-          if (!set_any(set, most > kGrow) || grown) break;
-          // the references of the rows that outgrow theirs move to the maximum of this step's scores; the others' stay, so that no row's
-          // numbers depend on another's
-          fence_after_sync();
+          // the references of the rows that outgrow theirs (of all, in the first step) move above the maximum of this step's scores; the
+          // others' stay, so that no row's numbers depend on another's
 #pragma unroll 1
           for (int i = 0; i < mine; ++i) {
-            uint32_t z[8];
-            tmem_ld8(s_addr + 8 * i, z);
-            wait_ld8(z);
+            uint64_t t[4];
+            scores(i, t, false);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              const float m = warp_max(valid ? __uint_as_float(z[c]) * kap[8 * i + c] : -INFINITY);
-              if (lane == 0) sm.red_max[set][quad][8 * i + c] = m;
+            for (int c = 0; c < 4; ++c) {
+              const float2 e = unpair64(t[c]);
+              const float m0 = warp_max(valid ? e.x : -INFINITY), m1 = warp_max(valid ? e.y : -INFINITY);
+              if (lane == 0) *reinterpret_cast<float2*>(&sm.red_max[set][quad][8 * i + 2 * c]) = make_float2(m0, m1);
             }
           }
-          if (j > 0 && quad == set) mbar_spin(&sm.o_done[b ^ 1], (uint32_t)((g - 1) >> 1), abort_flag);       // O^T so far is complete
+          if (j > 0 && quad == set) spin_for(&sm.o_done[b ^ 1], (g - 1) >> 1, abort_flag);                // O^T so far is complete
           set_sync(set);
           if (quad == 0 && lane < 8 * mine) {
             const float m = fmaxf(fmaxf(sm.red_max[set][0][lane], sm.red_max[set][1][lane]), fmaxf(sm.red_max[set][2][lane], sm.red_max[set][3][lane]));
-            const float old = -neg_ref[lane], to = m - old > kGrow ? m : old;
+            const float old = started ? -neg_ref[lane] : 0.f, top = m > -INFINITY ? m + kMargin : 0.f;
+            const float to = started && !(m - old > kGrow) ? old : top;
             neg_ref[lane] = -to;
             factor[lane] = to == old ? 1.f : fast_exp2(old - to);
           }
           set_sync(set);
-          if (j > 0) {
+          if (started) {
             fence_after_sync();
 #pragma unroll
-            for (int i = 0; i < 4 * kGroups; ++i)
-              if (i < 4 * mine) l[i] = mul2(l[i], *reinterpret_cast<const uint64_t*>(factor + 2 * i));
+            for (int i = 0; i < 4 * kGroups; ++i) {
+              if (i < 4 * mine) {
+                const uint64_t f = *reinterpret_cast<const uint64_t*>(factor + 2 * i);
+                l[i] = mul2(l[i], f);
+#pragma unroll
+                for (int v = 0; v < Gv; ++v) pb[v][i] = mul2(pb[v][i], f);
+              }
+            }
 #pragma unroll 1
-            for (int i = 0; i < mine * (Dv / 128); ++i) {
-              const uint32_t at = lane_addr + Sh::kColO + first + 8 * (i % mine) + kRows * (i / mine);
+            for (int i = 0; j > 0 && i < mine * (Dv / 128); ++i) {
+              const uint32_t at = lane_addr + Sh::kColO + 2 * kRows * (i / mine) + 2 * half * (quad >> 1) + first + 8 * (i % mine);
               uint32_t o[8];
               tmem_ld8(at, o);
               wait_ld8(o);
@@ -658,21 +737,27 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             wait_st();
             fence_before_sync();
           }
-          grown = true;
+          started = grown = true;
         }
         if (tid == 0) mbar_arrive(&sm.p_full[b]);
 #pragma unroll
-        for (int i = 0; i < 4 * kGroups; ++i)
-          if (i < 4 * mine) l[i] = add2(l[i], p[i]);
+        for (int i = 0; i < 4 * kGroups; ++i) {
+          if (i < 4 * mine) {
+            l[i] = add2(l[i], p[i]);
+#pragma unroll
+            for (int v = 0; v < Gv; ++v) pb[v][i] = fma2(p[i], vb[v], pb[v][i]);
+          }
+        }
       }
       // ---- the segment's record ----
-      if (quad == set) mbar_spin(&sm.o_done[(g - 1) & 1], (uint32_t)((g - 1) >> 1), abort_flag);
-      {
+      if (quad == set) spin_for(&sm.o_done[(g - 1) & 1], (g - 1) >> 1, abort_flag);
+#pragma unroll
+      for (int k = 0; k <= Gv; ++k) {
         float v[8 * kGroups];
 #pragma unroll
-        for (int i = 0; i < 4 * kGroups; ++i) { const float2 u = unpair64(l[i]); v[2 * i] = u.x; v[2 * i + 1] = u.y; }
+        for (int i = 0; i < 4 * kGroups; ++i) { const float2 u = unpair64(k == 0 ? l[i] : pb[k - 1][i]); v[2 * i] = u.x; v[2 * i + 1] = u.y; }
         const float sum = column_sums(v);
-        if (lane < 8 * kGroups) sm.red_sum[set][quad][lane] = sum;
+        if (lane < 8 * kGroups) sm.red_sum[set][quad][k][lane] = sum;
       }
       if (tid == 0) mbar_arrive(&sm.q_free[slot]);       // the set has passed a barrier since it last read kappa
       set_sync(set);
@@ -680,18 +765,18 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       const bool bad = *abort_flag || sm.poisoned[n % kInfo];
       float* o_out = P.rec_o + (size_t)s.record * Sh::kRecord;
       float2* ml = P.rec_ml + (size_t)s.record * kRows;
-      if (tid < 8 * mine && first + tid < rows)
-        ml[first + tid] = make_float2(-neg_ref[tid], bad ? -1.f : sm.red_sum[set][0][tid] + sm.red_sum[set][1][tid] + sm.red_sum[set][2][tid] + sm.red_sum[set][3][tid]);
+      auto total = [&](int k, int c) { return (sm.red_sum[set][0][k][c] + sm.red_sum[set][1][k][c]) + (sm.red_sum[set][2][k][c] + sm.red_sum[set][3][k][c]); };
+      if (tid < 8 * mine && first + tid < s.rows) ml[first + tid] = make_float2(-neg_ref[tid], bad ? -1.f : total(0, tid));
 #pragma unroll 1
       for (int i = 0; i < mine * (Dv / 128); ++i) {
-        const int row = first + 8 * (i % mine), m = i / mine;
+        const int m = i / mine, c0 = 8 * (i % mine);
         uint32_t o[8];
-        tmem_ld8(lane_addr + Sh::kColO + row + kRows * m, o);
+        tmem_ld8(lane_addr + Sh::kColO + 2 * kRows * m + 2 * half * (quad >> 1) + first + c0, o);
         wait_ld8(o);
-        float* at = o_out + (size_t)row * Dv + 128 * m + quad * 32 + lane;
+        float* at = o_out + (size_t)(first + c0) * Dv + 128 * m + quad * 32 + lane;
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          if (row + c < rows) at[c * Dv] = __uint_as_float(o[c]);
+          if (first + c0 + c < s.rows) at[c * Dv] = fmaf(__uint_as_float(o[c]), 16777216.f, total(1 + 2 * m + (quad >> 1), c0 + c));
       }
       fence_before_sync();
       set_sync(set);
@@ -706,7 +791,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     if (sm.abort_flag) {
       if (elect_one()) {                                 // the lane that issued the MMAs
         commit(&sm.drain);
-        for (uint32_t k = 0; k < kSpinLimit && !mbar_try_wait(&sm.drain, 0); ++k) {}
+    #pragma unroll 1
+    for (uint32_t k = 0; k < kSpinLimit && !mbar_try_wait(&sm.drain, 0); ++k) {}
         raise_flag(P.flags, Q4KV_FLAG_INTERNAL);
       }
       __syncwarp();
@@ -756,11 +842,12 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
   int parts = 0, record = 0, row = 0;                    // of the prefix: parts, the first one's record, the row in it
   if (fine && kv > 0 && mine.steps > 0) {
     const Cut cut(total, P.grid);
-    const int i = a - mine.agent0, t = ((i + 1) * mine.tiles - 1) / mine.n, segment = t * heads + head;
+    const int all = mine.n * n_rep, r = (a - mine.agent0) * n_rep + rep;
+    const int t = (int)(((long long)(r + 1) * mine.tiles - 1) / all), segment = t * heads + head;      // the tile that holds row r
     const int u = start + segment * mine.cost, c = cut.cta_of(u);
     parts = cut.cta_of(u + mine.steps - 1) - c + 1;
     record = tile0 * heads + segment + c;
-    row = (i - mine.n * t / mine.tiles) * n_rep + rep;
+    row = r - tile_begin(all, mine.tiles, t);
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int kQuads = Dv / 128;
@@ -817,17 +904,17 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
   if (lane == 0 && P.lse) P.lse[at] = zero ? -INFINITY : (M + log2f(L)) / kLog2e;
 }
 
-int max_rows_of(const Layout& y) { return y.D == 128 ? Shape<2, 2>::kRows : Shape<4, 4>::kRows; }
-static_assert(Shape<3, 2>::kRows == Shape<4, 4>::kRows, "");
+int max_rows_of(const Layout& y) { return y.D == 256 ? Shape<4, 4>::kRows : Shape<2, 2>::kRows; }
+static_assert(Shape<3, 2>::kRows == Shape<2, 2>::kRows, "");
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The workspace behind the header: the decode launch's records, what it leaves for the agents' own tokens, the prefixes' records (a CTA
-// leaves one per segment it touches).  Tiles: sum over groups of ceil(agents / agents of a tile) at most.
+// leaves one per segment it touches).  Tiles: sum over groups of ceil(rows / rows of a tile) at most.
 struct Sections { size_t own_lse, own_o, rec_ml, rec_o, end; };
 Sections sections_of(const Layout& y, int n_agents, int n_groups) {
-  const int rows = max_rows_of(y), most = rows / y.n_rep;
-  const size_t tiles = (size_t)n_agents / most + n_groups, records = tiles * y.Hkv + sm_count(), q_rows = (size_t)n_agents * y.Hq;
+  const int rows = max_rows_of(y);
+  const size_t tiles = (size_t)n_agents * y.n_rep / rows + n_groups, records = tiles * y.Hkv + sm_count(), q_rows = (size_t)n_agents * y.Hq;
   Sections s;
   s.own_lse = align256(decode_mma_workspace_bytes(y, n_agents));
   s.own_o = s.own_lse + align256(q_rows * sizeof(float));
@@ -883,8 +970,8 @@ cudaError_t launch_all(const Params& P, const q4kv_batch& b, void* ws, const Sec
 
 bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int max_kv_len) {
   // the list's positions are 32-bit numbers
-  return decode_mma_supported(y) && y.n_rep <= max_rows_of(y) && decode_mma_fits(y, n_agents, max_blocks) &&
-         2ll * n_agents * y.Hkv * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
+  return decode_mma_supported(y) && decode_mma_fits(y, n_agents, max_blocks) &&
+         (2ll * n_agents * y.Hq / max_rows_of(y) + n_agents * y.Hkv) * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
 }
 
 size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups) { return sections_of(y, n_agents, n_groups).end; }

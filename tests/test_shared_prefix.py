@@ -133,7 +133,7 @@ def test_against_each_agent_alone(shape, groups):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("shape", [(64, 1, 128, 128), (34, 2, 128, 128), (32, 1, 256, 256), (32, 1, 192, 128), (22, 2, 192, 128)])
+@pytest.mark.parametrize("shape", [(64, 1, 128, 128), (34, 2, 128, 128), (32, 1, 256, 256), (32, 1, 192, 128), (22, 2, 192, 128), (100, 1, 128, 128)])
 def test_many_query_heads_to_a_kv_head(shape):
     f = Forked(shape, [(333, [1, 50, 0]), (0, [20])], seed=32)
     q, scale = f.q(), 1.0 / math.sqrt(shape[2])
@@ -158,10 +158,9 @@ def test_bfloat16_scales_and_bfloat16_output(shape):
 @pytest.mark.parametrize("shape", [(16, 8, 128, 128), (32, 8, 128, 128), (8, 8, 192, 128), (16, 8, 256, 256)])
 def test_references_that_have_to_move(shape):
     """Scores that climb by thirty binary orders within 512 keys, again and again, with enough keys for several steps to a CTA: the
-    references of the rows' exponentials move, and what was added up before is scaled.  Against the attention over the keys and values
-    as the tiles hold them (each rounded once to binary16): what is left is the rounding of the probabilities, half a step or 2^-11
-    of each, so 2^-11 of the largest value in the numerator and in the denominator, and binary32 sums of scores of magnitude 30
-    (16 * 2^-24 * 30 < 1e-4 in an exponent)."""
+    references of the rows' exponentials move, and what was added up before is scaled.  Scores are exact up to binary32 sums (of
+    magnitude 30: 16 * 2^-24 * 30 < 1e-4 in an exponent); the probabilities times a value's scale are rounded once to binary16, half a
+    step or 2^-11 of p s c, and s c is at most the span of a group, twice the largest value."""
     def climb(f):
         n = f.lens[0]
         pos = np.arange(n)
@@ -182,7 +181,7 @@ def test_references_that_have_to_move(shape):
     qd, rep, most = synth.bf16_bits_to_f32(q).astype(np.float64), shape[0] // shape[1], 0.0
     for a, n in enumerate(f.lens):
         for h in range(shape[1]):
-            K, V = (x.astype(np.float16).astype(np.float64) for x in O.gather_dequant(f.opool, 0, f.tables[a], 0, n, h))
+            K, V = O.gather_dequant(f.opool, 0, f.tables[a], 0, n, h)
             s = scale * qd[a, h * rep:(h + 1) * rep] @ K.T
             top = s.max(1, keepdims=True)
             assert top.max() > 15.0
@@ -382,8 +381,7 @@ def test_refusals():
         assert call(**bad) == B.EINVAL, bad
     make = B.Spec.make
     for bad in (dict(sp=make(2, 8, 2, 64, 64)), dict(sp=make(2, 16, 1, 576, 512, True)), dict(sp=make(2, 8, 2, 128, 128, True)),
-                dict(sp=make(2, 130, 2, 128, 128)), dict(sp=make(2, 66, 2, 256, 256)), dict(sp=make(2, 33, 1, 192, 128)),
-                dict(sp=make(2, 8, 2, 128, 128, exact_products=True)), dict(scale=0.0), dict(scale=0.2), dict(scale=-0.1),
+                dict(sp=make(2, 8, 2, 192, 192)), dict(sp=make(2, 8, 2, 128, 128, exact_products=True)),
                 dict(agents=8193), dict(max_blocks=2**23), dict(agents=512, max_blocks=2**22, max_kv=0, sp=make(2, 64, 64, 128, 128))):
         assert call(**bad) == B.EUNSUPPORTED, bad
     need = B.q4kv_workspace_bytes_shared_prefix(spec, 2, 1024, 1)
