@@ -141,7 +141,7 @@ struct DecodeParams {
 };
 // kSingles: the batch of a prefill call, in which this launch takes the agents with exactly one query (row q_offs[a]).  An
 // instantiation of its own: the look-ups cost the others 1-4 % as a run-time branch.  kGroups: the agents of a group leave out the keys of
-// the group's prefix, which another launch attends.
+// the group's prefix, which another launch attends (or, with groups.whole, only have their lengths checked against it).
 enum class Batch { kAll, kSingles, kGroups };
 template <Batch kBatch>
 struct Params : DecodeParams {
@@ -177,7 +177,7 @@ __device__ inline AgentRange agent_range(const Par& P, int a, bool& bad) {
     bad = bad || P.groups.offs[g] > a || a >= P.groups.offs[g + 1] || prefix < 0 || (r.n > 0 && r.n < prefix);
   }
   if (bad) r.n = prefix = 0;
-  r.lo = Par::kGroups ? min(prefix, r.n) : window > 0 ? max(0, r.n - window) : 0;
+  r.lo = Par::kGroups ? (P.groups.whole ? 0 : min(prefix, r.n)) : window > 0 ? max(0, r.n - window) : 0;
   r.cf = r.lo >> 5;
   r.nc = r.n > r.lo ? ((r.n + 31) >> 5) - r.cf : 0;
   return r;
@@ -466,6 +466,7 @@ struct Smem {
   int fin[2][4];                                        // the CTA's first and last segment: pair, first CTA, last CTA, row
   int fin_last[2];                                      // this CTA drew the pair's last ticket
   int abort_flag;
+  int malformed;          // kGroups: offsets that do not ascend
 };
 
 // Online-softmax state of one warp for one segment.  A lane owns two score columns (2 tid, 2 tid + 1 of eight) and, of
@@ -957,13 +958,13 @@ __device__ __forceinline__ void combine_records(const DecodeParams& P, const flo
   if (d == 0 && P.lse) P.lse[row] = L > 0.f ? (M + log2f(L)) / kLog2e : -INFINITY;
 }
 
-// Agents first, first + step, ... without any key (kv_len == 0 or a rejected length): zeros, lse = -inf.
+// Agents first, first + step, ... without any key (kv_len == 0 or a rejected length), or all of them: zeros, lse = -inf.
 template <class Par>
-__device__ __forceinline__ void clear_empty_agents(const Par& P, int first, int step, int Dv, int lane) {
+__device__ __forceinline__ void clear_empty_agents(const Par& P, int first, int step, int Dv, int lane, bool all = false) {
 #pragma unroll 1
   for (int a = first; a < P.n_agents; a += step) {
     bool bad_len;
-    if (agent_range(P, a, bad_len).nc > 0 || (Par::kSingles && P.q_offs[a + 1] - P.q_offs[a] != 1)) continue;
+    if ((!all && agent_range(P, a, bad_len).nc > 0) || (Par::kSingles && P.q_offs[a + 1] - P.q_offs[a] != 1)) continue;
     const size_t row = Par::kSingles ? P.q_offs[a] : a;
 #pragma unroll 1
     for (int i = lane; i < P.y.Hq * Dv; i += 32) store_out(P, row * P.y.Hq * Dv + i, 0.f);
@@ -1042,6 +1043,12 @@ __global__ void __launch_bounds__(warps_of(G) * 32, kCtasPerSm) decode_mma_kerne
   } else {
     // columns of query heads that do not exist are never staged: they stay zero (factor 1)
     for (int i = threadIdx.x - 32; i < 2 * G * 32; i += (NW - 1) * 32) (&sm.qfrag[0][0])[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (Params<kBatch>::kGroups && warp == 1) {
+      bool bad = false;
+      for (int i = lane; i < P.groups.n; i += 32) bad |= P.groups.offs[i] < 0 || P.groups.offs[i + 1] < P.groups.offs[i] || P.groups.offs[i + 1] > P.n_agents;
+      bad = __any_sync(0xffffffffu, bad);
+      if (lane == 0) sm.malformed = bad;
+    }
     if (warp == NW - 1) {
       for (int i = lane; i < H * G; i += 32) (&sm.qsum[0][0])[i] = 0.f;
       if (lane < H) sm.kappa[lane] = 1.f;
@@ -1055,6 +1062,12 @@ __global__ void __launch_bounds__(warps_of(G) * 32, kCtasPerSm) decode_mma_kerne
     }
   }
   __syncthreads();
+  if (Params<kBatch>::kGroups && sm.malformed) {         // no agent's group is known
+    grid_dependency_wait();
+    if (cta == 0 && threadIdx.x == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
+    clear_empty_agents(P, cta * NW + warp, gridDim.x * NW, Dv, lane, true);
+    return;
+  }
   const int n_chunks = (int)(sm.range.u_end - sm.range.u_begin);
   const uint8_t* layer_base = P.pool + (uint64_t)P.layer * y.layer_bytes;
   uint32_t off = kOffBad;                                // pool offset of the warp's chunk number `lane` (of 32 at a time)
@@ -1393,7 +1406,7 @@ cudaError_t launch_decode_mma(const Layout& y, const void* pool, int n_blocks, i
   P.out = out; P.out_dtype = out_dtype; P.lse = lse; P.flags = flags;
   P.k_new = (const uint16_t*)k_new; P.v_new = (const uint16_t*)v_new;
   P.q_offs = q_offs;
-  P.groups = groups ? *groups : DecodeGroups{nullptr, nullptr, 0};
+  P.groups = groups ? *groups : DecodeGroups{nullptr, nullptr, 0, false};
   // No more CTAs than can be of use: one that finds nothing to do costs the next launch a microsecond, because its CTAs come in as
   // this one's leave.  No fewer than pairs, which one CTA would take in turn: a launch on contexts of 30 tokens took 25.5 us with
   // a CTA per eight chunks, 4.3 with one per pair, on 100 tokens 7.2 and 4.3, at d = 256 13.8 and 6.7.

@@ -133,5 +133,17 @@ __device__ inline void clear_tickets(const PrefillExtra& x) {
   for (int i = threadIdx.x; i < x.n_tickets; i += blockDim.x) x.tickets[i] = 0;
 }
 
+// The first agent of a0 .. a0 + n - 1 that holds `prefix` tokens; -1: none does (whole warp).
+__device__ inline int first_holder(const int32_t* lens, int a0, int n, int prefix, int max_kv_len) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int base = 0; base < n; base += 32) {
+    const int kv = base + lane < n ? lens[a0 + base + lane] : -1;
+    const unsigned has = __ballot_sync(0xffffffffu, kv >= prefix && kv > 0 && kv <= max_kv_len);
+    if (has) return a0 + base + __ffs(has) - 1;
+  }
+  return -1;
+}
+
 }  // namespace prefill
 }  // namespace q4kv

@@ -93,7 +93,8 @@ struct UmmaSmem {
   int abort_flag, poisoned;
 };
 
-template <bool kBf>
+// kGroups: see PrefillExtra::agent_lens
+template <bool kBf, bool kGroups>
 __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_constant__ UmmaParams P) {
   extern __shared__ __align__(128) uint8_t smem_raw[];
   UmmaSmem& sm = *reinterpret_cast<UmmaSmem*>(smem_raw);
@@ -106,16 +107,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // ---- this CTA's queries and key range (inputs no kernel writes) ----
-  const int q0 = P.q_offs[a], q_len = P.q_offs[a + 1] - q0;
+  const int q0 = P.q_offs[a], q_end = P.q_offs[a + 1];
+  const int q_len = kGroups && (q0 < 0 || q_end < q0 || q_end > P.x.n_agents) ? 0 : q_end - q0;
   const int kv_len = P.kv_lens[a];
   const int i_min = qt * 2 * tile_q;
   if (P.x.tickets && qt == 0 && blockIdx.y == 0 && a == 0) clear_tickets(P.x);
   if (i_min >= q_len || (P.x.tickets && q_len == 1)) return;   // uniform: nothing allocated, no barrier passed
-  const bool bad_len = kv_len < 0 || kv_len > P.max_blocks * kBlockTokens || q_len > kv_len;
+  const bool bad_len = kv_len < 0 || kv_len > (kGroups ? P.x.max_kv_len : P.max_blocks * kBlockTokens) || (!kGroups && q_len > kv_len);
   const int i_max = min(q_len, i_min + 2 * tile_q) - 1;
   const int prefix = kv_len - q_len;                     // query i sits at position prefix + i
-  const int W = P.window;
-  const int c_end = bad_len ? 0 : (prefix + i_max) / 32 + 1;
+  const int W = kGroups ? 0 : P.window;
+  const int c_end = bad_len ? 0 : kGroups ? (kv_len + 31) / 32 : (prefix + i_max) / 32 + 1;
   const int c_begin = (bad_len || W == 0) ? 0 : max(0, prefix + i_min - W + 1) >> 5;
   // steps of 128 keys (the last one may reach past the end, inside its pool block: zeros)
   const int all0 = c_begin >> 2, n_all = max(0, ((c_end + 3) >> 2) - all0);
@@ -150,17 +152,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_
     fewer_registers<kRegsOther>();
     if (warp == kLoadWarp) {
     // =============================== raw block loader ==========================================
+    const int reader = kGroups ? first_holder(P.x.agent_lens, q0, q_len, kv_len, P.x.max_kv_len) : a;        // -1: nobody needs the keys
     if (lane == 0) {
       int issued = 0;
       for (int j = 0; j < n_iter; ++j) {
         const int r = j % kRawSlots;
         if (j >= kRawSlots && !mbar_doze(&sm.raw_free[r], (uint32_t)(j / kRawSlots - 1), abort_flag)) break;
         const int c = 2 * (it0 + j);
-        const int blk = P.tables[(size_t)a * P.max_blocks + (c >> 3)];
+        const int blk = kGroups && reader < 0 ? -1 : P.tables[(size_t)reader * P.max_blocks + (c >> 3)];
         if (blk < 0 || blk >= P.n_blocks) {
           sm.bad[r] = 1;
           sm.poisoned = 1;
-          raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
+          if (!kGroups || reader >= 0) raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
           mbar_arrive(&sm.raw_full[r]);
         } else {
           sm.bad[r] = 0;
@@ -356,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_
     }
     const int h = row / tile_q, i = i_min + t * tile_q + row % tile_q;
     const bool mine = i < q_len && h < n_rep;            // (128 need not be a multiple of n_rep: the last rows are idle)
-    const int pq = prefix + i;                           // this row's position
+    const int pq = kGroups ? kv_len - 1 : prefix + i;    // this row's position
     const size_t row_index = (size_t)(q0 + i) * y.Hq + (size_t)hk * n_rep + h;
     float m_ref = -INFINITY, l = 0.f;                    // p = 2^(s - m_ref); m_ref trails the true maximum by at most 2^12
     for (int j = 0; j < n_step; ++j) {
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_
     if (ok) fence_after_sync();
     const bool bad = !ok || sm.poisoned != 0;
     const bool zero = bad || n_step == 0 || l <= 0.f;
-    const bool final = P.x.n_splits == 1;                // else the row is left as a record
+    const bool final = !kGroups && P.x.n_splits == 1;                // else the row is left as a record
     const float inv = zero ? 0.f : final ? 1.f / l : 1.f;
     // the warp's own query rows, which no product needs any more (another warp's may still be on their way here where the CTA has no keys)
     uint8_t* const buf = sm.qs[t] + (warp & 3) * 4 * 2048;
@@ -529,17 +532,19 @@ cudaError_t launch_prefill_umma(const Layout& y, const void* pool, int n_blocks,
   P.max_blocks = b.max_blocks; P.tables = b.block_tables; P.kv_lens = kv_lens; P.q_offs = q_offs; P.window = window;
   P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out; P.out_dtype = out_dtype; P.lse = lse; P.flags = flags;
   P.x = x;
-  static bool configured[64][2] = {};
+  static bool configured[64][4] = {};
   const size_t smem = sizeof(UmmaSmem);
-  const int bf = y.sb_bf16 ? 1 : 0;
-  void (*kernel)(const UmmaParams) = bf ? prefill_umma_kernel<true> : prefill_umma_kernel<false>;
+  const int form = (y.sb_bf16 ? 1 : 0) + (x.agent_lens ? 2 : 0);
+  void (*const kernels[4])(const UmmaParams) = {prefill_umma_kernel<false, false>, prefill_umma_kernel<true, false>,
+                                                prefill_umma_kernel<false, true>, prefill_umma_kernel<true, true>};
+  void (*kernel)(const UmmaParams) = kernels[form];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64 || !configured[dev][bf]) {
+  if (dev < 0 || dev >= 64 || !configured[dev][form]) {
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    if (dev >= 0 && dev < 64) configured[dev][bf] = true;
+    if (dev >= 0 && dev < 64) configured[dev][form] = true;
   }
   const int cta_q = 2 * (128 / y.n_rep);
   cudaLaunchConfig_t cfg = {};

@@ -100,7 +100,8 @@ struct UmmaSmem {
   int abort_flag, poisoned;
 };
 
-template <int G, int Gv, bool kBf>
+// kGroups: see PrefillExtra::agent_lens
+template <int G, int Gv, bool kBf, bool kGroups>
 __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const __grid_constant__ UmmaParams P) {
   using Sh = Shape<G, Gv>;
   constexpr int kD = Sh::D, kDv = Sh::Dv, kChunkBytes = Sh::kChunkBytes, kRawBytes = Sh::kRawBytes;
@@ -116,16 +117,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // ---- this CTA's queries and key range (inputs no kernel writes) ----
-  const int q0 = P.q_offs[a], q_len = P.q_offs[a + 1] - q0;
+  const int q0 = P.q_offs[a], q_end = P.q_offs[a + 1];
+  const int q_len = kGroups && (q0 < 0 || q_end < q0 || q_end > P.x.n_agents) ? 0 : q_end - q0;
   const int kv_len = P.kv_lens[a];
   const int i_min = qt * tile_q;
   if (P.x.tickets && qt == 0 && blockIdx.y == 0 && a == 0) clear_tickets(P.x);
   if (i_min >= q_len || (P.x.tickets && q_len == 1)) return;   // uniform: nothing allocated, no barrier passed
-  const bool bad_len = kv_len < 0 || kv_len > P.max_blocks * kBlockTokens || q_len > kv_len;
+  const bool bad_len = kv_len < 0 || kv_len > (kGroups ? P.x.max_kv_len : P.max_blocks * kBlockTokens) || (!kGroups && q_len > kv_len);
   const int i_max = min(q_len, i_min + tile_q) - 1;
   const int prefix = kv_len - q_len;                     // query i sits at position prefix + i
-  const int W = P.window;
-  const int c_end = bad_len ? 0 : (prefix + i_max) / 32 + 1;
+  const int W = kGroups ? 0 : P.window;
+  const int c_end = bad_len ? 0 : kGroups ? (kv_len + 31) / 32 : (prefix + i_max) / 32 + 1;
   const int c_begin = (bad_len || W == 0) ? 0 : max(0, prefix + i_min - W + 1) >> 5;
   const int all0 = c_begin >> 1, n_all = max(0, ((c_end + 1) >> 1) - all0);
   const int it0 = all0 + n_all * split / P.x.n_splits;   // 64-key blocks it0 .. it0 + n_iter - 1
@@ -162,17 +164,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
     fewer_registers<kRegsOther>();
     if (warp == kLoadWarp) {
       // =============================== raw block loader ==========================================
+      const int reader = kGroups ? first_holder(P.x.agent_lens, q0, q_len, kv_len, P.x.max_kv_len) : a;      // -1: nobody needs the keys
       if (lane == 0) {
         int issued = 0;
         for (int j = 0; j < n_iter; ++j) {
           const int r = j % kRawSlots;
           if (j >= kRawSlots && !mbar_wait(&sm.raw_free[r], (uint32_t)(j / kRawSlots - 1), abort_flag)) break;
           const int c = 2 * (it0 + j);
-          const int blk = P.tables[(size_t)a * P.max_blocks + (c >> 3)];
+          const int blk = kGroups && reader < 0 ? -1 : P.tables[(size_t)reader * P.max_blocks + (c >> 3)];
           if (blk < 0 || blk >= P.n_blocks) {
             sm.bad[r] = 1;
             sm.poisoned = 1;
-            raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
+            if (!kGroups || reader >= 0) raise_flag(P.flags, Q4KV_FLAG_BAD_BLOCK);
             mbar_arrive(&sm.raw_full[r]);
           } else {
             sm.bad[r] = 0;
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
     const int h = row / tile_q, i = i_min + row % tile_q;
     const bool mine = i < q_len && h < n_rep;            // (128 need not be a multiple of n_rep: the last rows are idle)
     const bool valid = mine && !bad_len;
-    const int pq = prefix + i;                           // this row's position
+    const int pq = kGroups ? kv_len - 1 : prefix + i;    // this row's position
     auto tile_barrier = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
     auto pair_any = [&](bool p) {                        // of the 64 threads of the rows' two warps
       uint32_t any;
@@ -525,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
     if (ok) fence_after_sync();
     const bool bad = !ok || sm.poisoned != 0;
     const bool zero = bad || n_iter == 0 || l <= 0.f;
-    const bool final = P.x.n_splits == 1;                // else the row is left as a record
+    const bool final = !kGroups && P.x.n_splits == 1;                // else the row is left as a record
     const float inv = zero ? 0.f : final ? 1.f / l : 1.f;
     const size_t row_index = (size_t)(q0 + i) * y.Hq + (size_t)hk * n_rep + h;
     const size_t at = final ? row_index * kDv : (row_index * P.x.n_splits + split) * prefill_record(kDv);
@@ -574,7 +577,7 @@ bool prefill_umma_1tile_supported(const Layout& y) {
 }
 
 namespace {
-template <int G, int Gv, bool kBf>
+template <int G, int Gv, bool kBf, bool kGroups>
 cudaError_t launch_shape(const UmmaParams& P, int max_q_len, cudaStream_t st) {
   static bool configured[64] = {};
   const size_t smem = sizeof(UmmaSmem<G, Gv>);
@@ -582,7 +585,7 @@ cudaError_t launch_shape(const UmmaParams& P, int max_q_len, cudaStream_t st) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(prefill_umma_1tile_kernel<G, Gv, kBf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(prefill_umma_1tile_kernel<G, Gv, kBf, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
@@ -597,7 +600,7 @@ cudaError_t launch_shape(const UmmaParams& P, int max_q_len, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, prefill_umma_1tile_kernel<G, Gv, kBf>, P);
+  return cudaLaunchKernelEx(&cfg, prefill_umma_1tile_kernel<G, Gv, kBf, kGroups>, P);
 }
 }  // namespace
 
@@ -611,8 +614,10 @@ cudaError_t launch_prefill_umma_1tile(const Layout& y, const void* pool, int n_b
   P.max_blocks = b.max_blocks; P.tables = b.block_tables; P.kv_lens = kv_lens; P.q_offs = q_offs; P.window = window;
   P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out; P.out_dtype = out_dtype; P.lse = lse; P.flags = flags;
   P.x = x;
-  if (y.D == 256) return y.sb_bf16 ? launch_shape<4, 4, true>(P, max_q_len, st) : launch_shape<4, 4, false>(P, max_q_len, st);
-  return y.sb_bf16 ? launch_shape<3, 2, true>(P, max_q_len, st) : launch_shape<3, 2, false>(P, max_q_len, st);
+  auto of = [&](auto launch_bf, auto launch_half) { return y.sb_bf16 ? launch_bf(P, max_q_len, st) : launch_half(P, max_q_len, st); };
+  if (x.agent_lens)
+    return y.D == 256 ? of(launch_shape<4, 4, true, true>, launch_shape<4, 4, false, true>) : of(launch_shape<3, 2, true, true>, launch_shape<3, 2, false, true>);
+  return y.D == 256 ? of(launch_shape<4, 4, true, false>, launch_shape<4, 4, false, false>) : of(launch_shape<3, 2, true, false>, launch_shape<3, 2, false, false>);
 }
 
 }  // namespace q4kv

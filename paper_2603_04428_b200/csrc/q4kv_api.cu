@@ -256,7 +256,7 @@ size_t q4kv_workspace_bytes_shared_prefix(const q4kv_spec* spec, int32_t n_agent
   const Layout y = make_layout(*spec, 1);
   const int agents = n_agents > 0 ? n_agents : 1;
   if (!shared_prefix_supported(y, agents, max_kv_len / kBlockTokens + 1, max_kv_len) || n_groups > agents) return 0;
-  return kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, agents, n_groups > 0 ? n_groups : 1);
+  return kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, agents, n_groups > 0 ? n_groups : 1, max_kv_len > 0 ? max_kv_len : 1);
 }
 
 int q4kv_shared_prefix_decode_attention(const q4kv_spec* spec, const void* pool, int32_t n_blocks, int32_t layer,
@@ -278,10 +278,10 @@ int q4kv_shared_prefix_decode_attention(const q4kv_spec* spec, const void* pool,
   if (max_kv_len == 0 || max_kv_len > cap) max_kv_len = cap;
   const Layout y = make_layout(*spec, n_blocks);
   if (!shared_prefix_supported(y, batch->n_agents, batch->max_blocks, max_kv_len) || spec->exact_products != 0) return Q4KV_EUNSUPPORTED;
-  if (workspace_bytes < kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, batch->n_agents, n_groups)) return Q4KV_EWORKSPACE;
+  if (workspace_bytes < kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, batch->n_agents, n_groups, max_kv_len)) return Q4KV_EWORKSPACE;
   const cudaError_t e = launch_shared_prefix(y, pool, n_blocks, layer, *batch, kv_lens, max_kv_len, group_offs, prefix_lens, n_groups, q,
-                                             softmax_scale, out, out_dtype, lse, workspace, status_flags,
-                                             (cudaStream_t)stream);
+                                             softmax_scale, tiles_allowed(spec, softmax_scale), out, out_dtype, lse, workspace,
+                                             workspace_bytes, status_flags, (cudaStream_t)stream);
   return e == cudaSuccess ? Q4KV_OK : Q4KV_ECUDA;
 }
 

@@ -137,8 +137,8 @@ cudaError_t launch_attention_generic(const Layout& y, const void* pool, int n_bl
                                      int max_kv_len, int window, const void* q, float scale, void* out,
                                      int out_dtype, float* lse, void* ws, int32_t* flags, cudaStream_t st);
 
-// Agents that share prefixes: group g holds agents offs[g] .. offs[g + 1] - 1 (device memory)
-struct DecodeGroups { const int32_t *offs, *prefix_lens; int n; };
+// Agents that share prefixes: group g holds agents offs[g] .. offs[g + 1] - 1 (device memory).  whole: the prefix is attended as well
+struct DecodeGroups { const int32_t *offs, *prefix_lens; int n; bool whole; };
 
 // tensor-core decode path (GQA shapes with d_qk = d_v in {128, 256}, and d_qk 192 with d_v 128)
 bool decode_mma_supported(const Layout& y);
@@ -151,7 +151,7 @@ cudaError_t launch_decode_mma(const Layout& y, const void* pool, int n_blocks, i
                               cudaStream_t st, const void* k_new = nullptr, const void* v_new = nullptr,
                               // q_offs: only the agents with exactly one query row; tickets: counters of their own
                               const int32_t* q_offs = nullptr, int32_t* tickets = nullptr,
-                              // groups: the keys before an agent's group's prefix_lens are left out
+                              // groups: lengths below the group's prefix are bad; the prefix's keys are left out (or not)
                               const DecodeGroups* groups = nullptr);
 int decode_mma_tickets(const Layout& y, int n_agents);
 
@@ -161,6 +161,11 @@ struct PrefillExtra {
   float* records;             // [total_q][Hq][n_splits][acc, m, l, pad]
   int32_t* tickets;           // arrival counters to clear for the decode launch that takes the agents with one query; or null
   int n_tickets;
+  // Groups of agents that share a prefix take the agents' place (d 128, d 256, 192 / 128): kv_lens holds the prefixes, q_offs the
+  // groups' agents, one query each, every query attends the whole prefix, always into records.  agent_lens: the agents' lengths (the
+  // prefix is read through the first agent that has it), or null; at most max_kv_len each
+  const int32_t* agent_lens;
+  int n_agents, max_kv_len;
 };
 
 // tensor-core prefill path (d_qk = d_v = 128, at most 4 query heads per KV head)
@@ -207,10 +212,11 @@ cudaError_t launch_merge_prefill(const Layout& y, int total_q, int n_splits, con
 
 // Decode of agents that share prefixes (d_qk = d_v in {128, 256}, d_qk 192 / d_v 128)
 bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int max_kv_len);
-size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups);
+size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len);
 cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
                                  int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
-                                 float scale, void* out, int out_dtype, float* lse, void* workspace, int32_t* flags, cudaStream_t st);
+                                 float scale, bool tiles_allowed, void* out, int out_dtype, float* lse, void* workspace,
+                                 size_t workspace_bytes, int32_t* flags, cudaStream_t st);
 
 // Decode on the MLA-latent cache (d_qk 576, d_v 512 aliasing K, one KV head, at most 16 query heads): a key-split
 // attention kernel -- on a binary16 tile of the dequantized keys, or, with on_codes, on the 4-bit codes themselves

@@ -85,6 +85,8 @@ struct Params {
   int32_t* flags;
   float* rec_o;               // [record][row][d_v]
   float2* rec_ml;             // [record][row]: m, l
+  const float* tile_records;  // instead, where the prefill kernel takes the prefixes: [agent][query head][splits][o, m, l, pad]
+  int splits;
   const float* own_o;         // [agent][query head][d_v]: of the agents' own tokens, normalised
   const float* own_lse;       // [agent][query head]
   CodeMasks masks;
@@ -839,15 +841,24 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
   const int kv = P.kv_lens[a];
   const bool fine = ascending && found && kv >= 0 && kv <= P.max_kv_len && (kv == 0 || kv >= mine.prefix);
   if (!fine && lane == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
-  int parts = 0, record = 0, row = 0;                    // of the prefix: parts, the first one's record, the row in it
-  if (fine && kv > 0 && mine.steps > 0) {
+  int parts = 0;                                         // of the prefix
+  const float *rec = P.rec_o, *rec_ml = (const float*)P.rec_ml;             // of the first part, then `stride` / `ml_stride` floats further
+  size_t stride = (size_t)kRows * Dv, ml_stride = 2 * kRows;
+  if (fine && kv > 0 && mine.steps > 0 && P.splits > 0) {
+    parts = P.splits;
+    stride = ml_stride = prefill_record(Dv);
+    rec = P.tile_records + (size_t)at * parts * stride;
+    rec_ml = rec + Dv;
+  } else if (fine && kv > 0 && mine.steps > 0) {
     const Cut cut(total, P.grid);
     const int all = mine.n * n_rep, r = (a - mine.agent0) * n_rep + rep;
     const int t = (int)(((long long)(r + 1) * mine.tiles - 1) / all), segment = t * heads + head;      // the tile that holds row r
     const int u = start + segment * mine.cost, c = cut.cta_of(u);
     parts = cut.cta_of(u + mine.steps - 1) - c + 1;
-    record = tile0 * heads + segment + c;
-    row = r - tile_begin(all, mine.tiles, t);
+    const int record = tile0 * heads + segment + c;
+    const int row = r - tile_begin(all, mine.tiles, t);
+    rec += (size_t)record * stride + (size_t)row * Dv;
+    rec_ml += (size_t)record * ml_stride + 2 * row;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int kQuads = Dv / 128;
@@ -868,9 +879,9 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
   for (int base = 0; base < parts; base += 32) {
     const int n = min(32, parts - base);
     float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < n) ml = __ldcg(P.rec_ml + (size_t)(record + base + lane) * kRows + row);
+    if (lane < n) ml = __ldcg(reinterpret_cast<const float2*>(rec_ml + (base + lane) * ml_stride));
     bad |= __any_sync(0xffffffffu, ml.y < 0.f) != 0;
-    const float* o = P.rec_o + ((size_t)(record + base) * kRows + row) * Dv + 4 * lane;
+    const float* o = rec + base * stride + 4 * lane;
     const float m = fmaxf(M, warp_max(ml.x));
     const float keep = M == -INFINITY ? 0.f : fast_exp2(M - m), e = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
     L = L * keep + warp_sum(e * ml.y);
@@ -882,7 +893,7 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
       const float f = __shfl_sync(0xffffffffu, e, j);
 #pragma unroll
       for (int k = 0; k < kQuads; ++k) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + (size_t)j * kRows * Dv + 128 * k));
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + j * stride + 128 * k));
         acc[k].x = fmaf(f, v.x, acc[k].x); acc[k].y = fmaf(f, v.y, acc[k].y); acc[k].z = fmaf(f, v.z, acc[k].z); acc[k].w = fmaf(f, v.w, acc[k].w);
       }
     }
@@ -909,18 +920,42 @@ static_assert(Shape<3, 2>::kRows == Shape<2, 2>::kRows, "");
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// How a call is computed, by what the host knows of it.
+//   kAlone: every agent by itself, one launch of the decode kernel.  kList: the prefixes by the kernel above.  kTiles: by the prefill
+//   kernel, which expands a block once for 256 score rows (128 at d = 256 and 192 / 128) instead of unpacking it for 32.
+enum class Route { kAlone, kList, kTiles };
+Route route_of(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool tiles_allowed) {
+  if (n_groups >= n_agents) return Route::kAlone;        // nothing is shared
+  const long long rows = (long long)n_agents * y.n_rep / n_groups;           // of an average group and KV head
+  if (tiles_allowed && rows > 64 && (prefill_umma_supported(y) || prefill_umma_1tile_supported(y))) return Route::kTiles;
+  return Route::kList;
+}
+// The launch of the prefill kernel: groups take the agents' place
+int tile_queries(const Layout& y) { return prefill_umma_supported(y) ? 2 * (128 / y.n_rep) : 128 / y.n_rep; }
+int tile_splits(const Layout& y, int n_agents, int n_groups, int max_kv_len, size_t bytes) {
+  return plan_prefill_splits(y, tile_queries(y), 1, n_groups, n_agents, (n_agents + n_groups - 1) / n_groups, max_kv_len, 0, bytes);
+}
+
 // The workspace behind the header: the decode launch's records, what it leaves for the agents' own tokens, the prefixes' records (a CTA
-// leaves one per segment it touches).  Tiles: sum over groups of ceil(rows / rows of a tile) at most.
+// of the list leaves one per segment it touches).  Tiles: sum over groups of ceil(rows / rows of a tile) at most.
 struct Sections { size_t own_lse, own_o, rec_ml, rec_o, end; };
-Sections sections_of(const Layout& y, int n_agents, int n_groups) {
-  const int rows = max_rows_of(y);
-  const size_t tiles = (size_t)n_agents * y.n_rep / rows + n_groups, records = tiles * y.Hkv + sm_count(), q_rows = (size_t)n_agents * y.Hq;
+Sections sections_of(const Layout& y, int n_agents, int n_groups, int max_kv_len, Route route) {
+  const size_t q_rows = (size_t)n_agents * y.Hq;
   Sections s;
   s.own_lse = align256(decode_mma_workspace_bytes(y, n_agents));
   s.own_o = s.own_lse + align256(q_rows * sizeof(float));
   s.rec_ml = s.own_o + align256(q_rows * y.Dv * sizeof(float));
-  s.rec_o = s.rec_ml + align256(records * rows * sizeof(float2));
-  s.end = s.rec_o + align256(records * rows * y.Dv * sizeof(float));
+  if (route == Route::kAlone) {
+    s.rec_ml = s.rec_o = s.end = s.own_lse;
+  } else if (route == Route::kTiles) {
+    s.rec_o = s.rec_ml;
+    s.end = s.rec_o + align256(prefill_record_bytes(y, n_agents, tile_splits(y, n_agents, n_groups, max_kv_len, (size_t)-1)));
+  } else {
+    const int rows = max_rows_of(y);
+    const size_t tiles = q_rows / y.Hkv / rows + n_groups, records = tiles * y.Hkv + sm_count();
+    s.rec_o = s.rec_ml + align256(records * rows * sizeof(float2));
+    s.end = s.rec_o + align256(records * rows * y.Dv * sizeof(float));
+  }
   return s;
 }
 
@@ -955,15 +990,12 @@ cudaError_t launch_prefixes(const Params& P, cudaStream_t st) {
   return launch_pdl(shared_prefix_kernel<G, Gv, kBf>, P.grid, kThreads, smem, st, P);
 }
 template <int G, int Gv>
-cudaError_t launch_all(const Params& P, const q4kv_batch& b, void* ws, const Sections& s, float scale, cudaStream_t st) {
-  cudaError_t e = P.y.sb_bf16 ? launch_prefixes<G, Gv, true>(P, st) : launch_prefixes<G, Gv, false>(P, st);
-  if (e != cudaSuccess) return e;
-  const DecodeGroups groups = {P.group_offs, P.prefix_lens, P.n_groups};
-  const int no_window = 0;
-  e = launch_decode_mma(P.y, P.pool, P.n_blocks, P.layer, b, P.kv_lens, P.max_kv_len, &no_window, 1, P.q, scale, (void*)P.own_o,
-                        Q4KV_OUT_F32, (float*)P.own_lse, ws, P.flags, st, nullptr, nullptr, nullptr, nullptr, &groups);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(shared_prefix_merge_kernel<64 * Gv, Shape<G, Gv>::kRows>, (P.n_agents * P.y.Hq + 3) / 4, 128, 0, st, P);
+cudaError_t launch_list(const Params& P, cudaStream_t st) {
+  return P.y.sb_bf16 ? launch_prefixes<G, Gv, true>(P, st) : launch_prefixes<G, Gv, false>(P, st);
+}
+template <int Dv, int kRows>
+cudaError_t launch_merge(const Params& P, cudaStream_t st) {
+  return launch_pdl(shared_prefix_merge_kernel<Dv, kRows>, (P.n_agents * P.y.Hq + 3) / 4, 128, 0, st, P);
 }
 
 }  // namespace
@@ -974,23 +1006,52 @@ bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int 
          (2ll * n_agents * y.Hq / max_rows_of(y) + n_agents * y.Hkv) * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
 }
 
-size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups) { return sections_of(y, n_agents, n_groups).end; }
+size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len) {
+  size_t most = 0;                                       // whatever the softmax scale
+  for (const bool tiles : {false, true}) {
+    const size_t end = sections_of(y, n_agents, n_groups, max_kv_len, route_of(y, n_agents, n_groups, max_kv_len, tiles)).end;
+    if (end > most) most = end;
+  }
+  return most;
+}
 
 // workspace: with its header (the decode launch's arrival counters)
 cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
                                  int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
-                                 float scale, void* out, int out_dtype, float* lse, void* workspace, int32_t* flags, cudaStream_t st) {
-  const Sections s = sections_of(y, b.n_agents, n_groups);
+                                 float scale, bool tiles_allowed, void* out, int out_dtype, float* lse, void* workspace,
+                                 size_t workspace_bytes, int32_t* flags, cudaStream_t st) {
+  const Route route = route_of(y, b.n_agents, n_groups, max_kv_len, tiles_allowed);
+  const int no_window = 0;
+  if (route == Route::kAlone) {
+    const DecodeGroups whole = {group_offs, prefix_lens, n_groups, true};
+    return launch_decode_mma(y, pool, n_blocks, layer, b, kv_lens, max_kv_len, &no_window, 1, q, scale, out, out_dtype, lse, workspace,
+                             flags, st, nullptr, nullptr, nullptr, nullptr, &whole);
+  }
+  const Sections s = sections_of(y, b.n_agents, n_groups, max_kv_len, route);
   uint8_t* at = (uint8_t*)workspace + kWorkspaceHeaderBytes;
   Params P;
   P.y = y; P.pool = (const uint8_t*)pool; P.n_blocks = n_blocks; P.layer = layer; P.n_agents = b.n_agents; P.max_blocks = b.max_blocks;
   P.tables = b.block_tables; P.kv_lens = kv_lens; P.max_kv_len = max_kv_len; P.group_offs = group_offs; P.prefix_lens = prefix_lens;
   P.n_groups = n_groups; P.grid = sm_count(); P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out;
   P.out_dtype = out_dtype; P.lse = lse; P.flags = flags; P.own_lse = (float*)(at + s.own_lse); P.own_o = (float*)(at + s.own_o);
-  P.rec_ml = (float2*)(at + s.rec_ml); P.rec_o = (float*)(at + s.rec_o);
-  if (y.D == 128) return launch_all<2, 2>(P, b, workspace, s, scale, st);
-  if (y.D == 256) return launch_all<4, 4>(P, b, workspace, s, scale, st);
-  return launch_all<3, 2>(P, b, workspace, s, scale, st);
+  P.rec_ml = (float2*)(at + s.rec_ml); P.rec_o = (float*)(at + s.rec_o); P.tile_records = P.rec_o; P.splits = 0;
+  cudaError_t e;
+  if (route == Route::kTiles) {
+    PrefillExtra x = {};
+    P.splits = x.n_splits = tile_splits(y, b.n_agents, n_groups, max_kv_len, workspace_bytes - kWorkspaceHeaderBytes - s.rec_o);
+    x.records = P.rec_o; x.agent_lens = kv_lens; x.n_agents = b.n_agents; x.max_kv_len = max_kv_len;
+    const q4kv_batch groups = {n_groups, b.max_blocks, b.block_tables};
+    const auto launch = prefill_umma_supported(y) ? launch_prefill_umma : launch_prefill_umma_1tile;
+    e = launch(y, pool, n_blocks, layer, groups, prefix_lens, group_offs, b.n_agents, 0, q, scale, nullptr, Q4KV_OUT_F32, nullptr, flags, st, x);
+  } else {
+    e = y.D == 128 ? launch_list<2, 2>(P, st) : y.D == 256 ? launch_list<4, 4>(P, st) : launch_list<3, 2>(P, st);
+  }
+  if (e != cudaSuccess) return e;
+  const DecodeGroups own = {group_offs, prefix_lens, n_groups, false};
+  e = launch_decode_mma(y, pool, n_blocks, layer, b, kv_lens, max_kv_len, &no_window, 1, q, scale, (void*)P.own_o, Q4KV_OUT_F32,
+                        (float*)P.own_lse, workspace, flags, st, nullptr, nullptr, nullptr, nullptr, &own);
+  if (e != cudaSuccess) return e;
+  return y.D == 256 ? launch_merge<256, Shape<4, 4>::kRows>(P, st) : launch_merge<128, Shape<2, 2>::kRows>(P, st);
 }
 
 }  // namespace q4kv

@@ -13,11 +13,11 @@ ATOL, RTOL_ROW = 2e-3, 1e-2      # the library's parity bounds for unit-variance
 
 
 class Forked:
-    """Groups [(prefix, [own tokens or None for an idle agent])] as an oracle pool and a device pool.  On the device, what the call
-    must not read is poison: table entries of whole prefix blocks and the prefix's tokens in the copied block (agents but the first with
-    tokens), and every slot past a length."""
+    """Groups [(prefix, [own tokens or None for an idle agent])] as an oracle pool and a device pool, where every slot past a length is
+    poison.  wide: entries of a block-table row.  Which way a call takes is chosen by what the host knows, the number of agents and
+    groups and the width of the rows: wide rows stand for long contexts, where prefixes are attended once for their group."""
 
-    def __init__(self, shape, groups, seed, sb_dtype=0, layers=1, edit=None):
+    def __init__(self, shape, groups, seed, sb_dtype=0, layers=1, edit=None, wide=1):
         from paper_2603_04428_b200 import harness as H
         hq, hkv, d, dv = shape
         self.shape, self.groups = shape, groups
@@ -31,7 +31,7 @@ class Forked:
             lead = None
             for t in tails:
                 if t is None:
-                    rows.append(([], []))
+                    rows.append([])
                     lens.append(0)
                     continue
                 mine = list(range(n, n + -(-(prefix + t) // 256) - whole))
@@ -39,21 +39,17 @@ class Forked:
                 first = lead is None
                 if part and not first:
                     copies.append((lead[whole], mine[0], part))
-                    poison.append((mine[0], 0, part))
                 elif first:
                     lead = shared + mine
                 if (prefix + t) % 256:
                     poison.append(((shared + mine)[-1], (prefix + t) % 256, 256))
-                rows.append((shared + mine, (shared if first else [-1] * whole) + mine))
+                rows.append(shared + mine)
                 lens.append(prefix + t)
         self.n_blocks = n + 2
         order = g.permutation(self.n_blocks)
-        wide = max(1, max(len(r[0]) for r in rows))
-        real = np.full((len(rows), wide), -1, np.int32)
-        told = real.copy()
-        for i, (a, b) in enumerate(rows):
+        real = np.full((len(rows), max([wide] + [len(r) for r in rows])), -1, np.int32)
+        for i, a in enumerate(rows):
             real[i, :len(a)] = [order[x] for x in a]
-            told[i, :len(b)] = [order[x] if x >= 0 else -1 for x in b]
         self.lens, self.tables = lens, real
         self.offs = np.concatenate([[0], np.cumsum([len(t) for _, t in groups])]).astype(np.int32)
         self.prefix = [p for p, _ in groups]
@@ -79,7 +75,7 @@ class Forked:
         image = O.pack(self.opool, np.arange(self.n_blocks), self.n_blocks * 256)
         for t, c in zip(self.opool.tensors(), clean):
             t[:] = c
-        self.dc = H.DeviceCache(layers, hq, hkv, d, dv, False, self.n_blocks, told, sb_dtype=sb_dtype)
+        self.dc = H.DeviceCache(layers, hq, hkv, d, dv, False, self.n_blocks, real, sb_dtype=sb_dtype)
         B.q4kv_unpack(self.dc.spec, H.dev(image), self.n_blocks * 256, self.dc.pool, self.n_blocks,
                       H.dev(np.arange(self.n_blocks, dtype=np.int32)), self.dc.flags)
 
@@ -119,32 +115,38 @@ GROUPS = {
 }
 
 
+WIDE = 2048                      # rows of 524288 tokens
+
+
 @pytest.mark.gpu
+@pytest.mark.parametrize("wide", [1, WIDE])
 @pytest.mark.parametrize("groups", list(GROUPS))
 @pytest.mark.parametrize("shape", [(8, 2, 128, 128), (3, 1, 128, 128), (4, 4, 128, 128), (8, 1, 128, 128), (2, 2, 192, 128),
                                    (4, 2, 256, 256), (5, 1, 256, 256)])
-def test_against_each_agent_alone(shape, groups):
-    f = Forked(shape, GROUPS[groups], seed=31)
-    scale = 1.0 / math.sqrt(shape[2])
+def test_against_each_agent_alone(shape, groups, wide):
+    f = Forked(shape, GROUPS[groups], seed=31, wide=wide)
     q = f.q()
-    out, lse = f.run(q, scale)
-    close(out, lse, *f.want(q, scale))
+    for sharp in (1.0, 2.5):                             # a scale above 2 / sqrt(d) does not go to tiles rounded to binary16
+        scale = sharp / math.sqrt(shape[2])
+        out, lse = f.run(q, scale)
+        close(out, lse, *f.want(q, scale))
     assert f.dc.read_flags() == 0
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", [(64, 1, 128, 128), (34, 2, 128, 128), (32, 1, 256, 256), (32, 1, 192, 128), (22, 2, 192, 128), (100, 1, 128, 128)])
 def test_many_query_heads_to_a_kv_head(shape):
-    f = Forked(shape, [(333, [1, 50, 0]), (0, [20])], seed=32)
+    f = Forked(shape, [(333, [1, 50, 0]), (0, [20])], seed=32, wide=WIDE)
     q, scale = f.q(), 1.0 / math.sqrt(shape[2])
     out, lse = f.run(q, scale)
     close(out, lse, *f.want(q, scale))
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("groups", [[(700, [1, 90, 300]), (40, [5])], [(700, [i % 5 for i in range(70)])]])
 @pytest.mark.parametrize("shape", [(8, 2, 128, 128), (2, 2, 192, 128), (4, 2, 256, 256)])
-def test_bfloat16_scales_and_bfloat16_output(shape):
-    f = Forked(shape, [(700, [1, 90, 300]), (40, [5])], seed=33, sb_dtype=1, layers=2)
+def test_bfloat16_scales_and_bfloat16_output(shape, groups):
+    f = Forked(shape, groups, seed=33, sb_dtype=1, layers=2, wide=WIDE)
     q, scale = f.q(), 1.0 / math.sqrt(shape[2])
     for layer in range(2):
         out, lse = f.run(q, scale, layer=layer)
@@ -172,7 +174,7 @@ def test_references_that_have_to_move(shape):
             c, s, b = O.quantize_rows(synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(x)))
             f.opool.Kc[at], f.opool.Ks[at], f.opool.Kb[at] = O.pack_codes(c), s, b
 
-    f = Forked(shape, [(20000, [40, 0, 200])], seed=34, edit=climb)
+    f = Forked(shape, [(20000, [40, 0, 200])], seed=34, edit=climb, wide=WIDE)
     qf = synth.bf16_bits_to_f32(f.q())
     qf[..., 0] = 4.0 + np.abs(qf[..., 0])                # every query has a part along the climbing element
     q, scale = synth.f32_to_bf16_bits(qf), 1.0 / math.sqrt(shape[2])
@@ -192,8 +194,9 @@ def test_references_that_have_to_move(shape):
 
 
 @pytest.mark.gpu
-def test_one_agents_bad_query_leaves_the_others_alone():
-    f = Forked((8, 2, 128, 128), [(600, [20, 30, 1, 0])], seed=35)
+@pytest.mark.parametrize("more", [0, 60])
+def test_one_agents_bad_query_leaves_the_others_alone(more):
+    f = Forked((8, 2, 128, 128), [(600, [20, 30, 1, 0] + [2] * more)], seed=35, wide=WIDE)
     q, scale = f.q(), 1.0 / math.sqrt(128)
     good, _ = f.run(q, scale)
     bad = q.copy()
@@ -210,11 +213,12 @@ def test_one_agents_bad_query_leaves_the_others_alone():
 
 
 @pytest.mark.gpu
-def test_lengths_that_cannot_be_raise_the_flag_and_give_zeros():
-    f = Forked((8, 2, 128, 128), [(300, [20, 30, 9]), (40, [100, 3])], seed=36)
+@pytest.mark.parametrize("wide, more", [(1, 0), (WIDE, 0), (WIDE, 80)])
+def test_lengths_that_cannot_be_raise_the_flag_and_give_zeros(wide, more):
+    f = Forked((8, 2, 128, 128), [(300, [20, 30, 9]), (40, [100, 3] + [1] * more)], seed=36, wide=wide)
     q, scale = f.q(), 1.0 / math.sqrt(128)
     good, good_lse = f.run(q, scale)
-    width = f.tables.shape[1] * 256
+    width, A = f.tables.shape[1] * 256, len(f.lens)
 
     def call(lens=None, offs=None, prefix=None, **kw):
         f.dc.flags.zero_()
@@ -229,43 +233,44 @@ def test_lengths_that_cannot_be_raise_the_flag_and_give_zeros():
         lens = list(f.lens)
         lens[a] = n
         out, lse, flag = call(lens=lens)
-        # (another agent leads the first group's prefix when its first one is out: here, one whose row has no entries for it)
-        rest = [i for i in range(5) if i != a] if a else [3, 4]
-        assert flag == (B.FLAG_BAD_LENGTH if a else B.FLAG_BAD_LENGTH | B.FLAG_BAD_BLOCK)
-        assert torch.all(out[a] == 0) and torch.all(torch.isneginf(lse[a])) and near(out, good, rest)
+        rest = [i for i in range(A) if i != a]
+        assert flag == B.FLAG_BAD_LENGTH and torch.all(out[a] == 0) and torch.all(torch.isneginf(lse[a])) and near(out, good, rest)
     out, lse, flag = call(max_kv_len=325)
-    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[1] == 0) and near(out, good, [0, 2, 3, 4])
+    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[1] == 0) and near(out, good, [0] + list(range(2, A)))
     for prefix in ([-1, 40], [width + 1, 40]):
         out, lse, flag = call(prefix=prefix)
-        assert flag == B.FLAG_BAD_LENGTH and torch.all(out[:3] == 0) and near(out, good, [3, 4])
-    for offs in ([0, 4, 3], [-1, 3, 5], [0, 3, 6], [0, 3, 2**31 - 1], [5, 3, 0]):
+        assert flag == B.FLAG_BAD_LENGTH and torch.all(out[:3] == 0) and near(out, good, list(range(3, A)))
+    for offs in ([0, 4, 3], [-1, 3, A], [0, 3, A + 1], [0, 3, 2**31 - 1], [A, 3, 0]):
         out, lse, flag = call(offs=offs)
         assert flag == B.FLAG_BAD_LENGTH and torch.all(out == 0) and torch.all(torch.isneginf(lse)), offs
-    out, lse, flag = call(offs=[0, 3, 4])                # the last agent belongs to no group
-    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[4] == 0) and near(out, good, [0, 1, 2, 3])
-    out, lse, flag = call(offs=[3, 3, 5])
+    out, lse, flag = call(offs=[0, 3, 4])                # the agents from 4 on belong to no group
+    assert flag == B.FLAG_BAD_LENGTH and torch.all(out[4:] == 0) and near(out, good, [0, 1, 2, 3])
+    out, lse, flag = call(offs=[3, 3, A])
     assert flag == B.FLAG_BAD_LENGTH and torch.all(out[:3] == 0)
     out, lse, flag = call()
     assert flag == 0 and torch.equal(out, good) and torch.equal(lse, good_lse)
 
 
 @pytest.mark.gpu
-def test_bad_blocks_spoil_the_group_or_the_agent():
-    f = Forked((8, 2, 128, 128), [(600, [20, 300, 9]), (40, [100, 3])], seed=37)
+@pytest.mark.parametrize("wide, more", [(1, 0), (WIDE, 0), (WIDE, 80)])
+def test_bad_blocks_spoil_the_agents_that_read_them(wide, more):
+    f = Forked((8, 2, 128, 128), [(600, [20, 300, 9] + [1] * more), (40, [100, 3])], seed=37, wide=wide)
     q, scale = f.q(), 1.0 / math.sqrt(128)
     good, _ = f.run(q, scale)
-    keep = f.dc.tables.clone()
+    keep, A, n = f.dc.tables.clone(), len(f.lens), 3 + more
     for bad in (-1, f.n_blocks, 2**31 - 1, -2**31):
         f.dc.tables.copy_(keep)
-        f.dc.tables[0, 1] = bad                          # read for the whole group
+        f.dc.tables[0, 1] = bad                          # of the prefix, which the whole group reads through this row, or this agent alone
         out, lse = f.run(q, scale)
-        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[:3] == 0) and torch.all(torch.isneginf(lse[:3]))
-        assert torch.equal(out[3:], good[3:])
+        k = n
+        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[:k] == 0) and torch.all(torch.isneginf(lse[:k]))
+        assert torch.equal(out[k:], good[k:])
         f.dc.flags.zero_()
         f.dc.tables.copy_(keep)
         f.dc.tables[1, 3] = bad
         out, lse = f.run(q, scale)
-        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[1] == 0) and torch.equal(out[[0, 2, 3, 4]], good[[0, 2, 3, 4]])
+        rest = [0] + list(range(2, A))
+        assert f.dc.read_flags() == B.FLAG_BAD_BLOCK and torch.all(out[1] == 0) and torch.equal(out[rest], good[rest])
         f.dc.flags.zero_()
 
 
@@ -274,12 +279,13 @@ def test_the_largest_batch_and_runs_that_repeat():
     """512 agents in uneven groups; the same bits every time, from a workspace that other calls have used, eager and replayed."""
     r = np.random.default_rng(4)
     sizes = [200, 1, 100, 64, 33, 114]
-    f = Forked((2, 1, 128, 128), [(int(r.integers(0, 700)), [int(x) for x in r.integers(0, 60, n)]) for n in sizes], seed=38)
+    f = Forked((2, 1, 128, 128), [(int(r.integers(0, 700)), [int(x) for x in r.integers(0, 60, n)]) for n in sizes], seed=38, wide=WIDE)
     q, scale = f.q(), 1.0 / math.sqrt(128)
     out, lse = f.run(q, scale)
     close(out, lse, *f.want(q, scale))
     A, spec, dc = 512, f.dc.spec, f.dc
-    need = max(B.q4kv_workspace_bytes_shared_prefix(spec, A, 1024, 6), B.q4kv_workspace_bytes(spec, A, 1024, 0))
+    most = WIDE * 256
+    need = max(B.q4kv_workspace_bytes_shared_prefix(spec, A, most, 6), B.q4kv_workspace_bytes(spec, A, most, 0))
     ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
     ws[:B.WORKSPACE_HEADER_BYTES] = 0
     from paper_2603_04428_b200 import harness as H
@@ -287,7 +293,7 @@ def test_the_largest_batch_and_runs_that_repeat():
     o2, l2 = torch.empty_like(out), torch.empty_like(lse)
 
     def call():
-        B.q4kv_shared_prefix_decode_attention(spec, dc.pool, f.n_blocks, 0, dc.bt, lens, 1024, offs, pre, 6, qd, scale, o2, B.OUT_F32,
+        B.q4kv_shared_prefix_decode_attention(spec, dc.pool, f.n_blocks, 0, dc.bt, lens, most, offs, pre, 6, qd, scale, o2, B.OUT_F32,
                                               l2, ws, dc.flags)
     call()
     assert torch.equal(o2, out) and torch.equal(l2, lse) and int(ws[:B.WORKSPACE_HEADER_BYTES].max()) == 0
@@ -303,7 +309,6 @@ def test_the_largest_batch_and_runs_that_repeat():
     torch.cuda.synchronize()
     assert torch.equal(o2, out) and torch.equal(l2, lse)
     gone = torch.arange(A, device="cuda") % 3 == 0       # the replay reads the lengths of the moment
-    gone[f.offs[:-1]] = False                            # (the groups' first agents stay: only their rows hold the prefix here)
     lens.copy_(torch.where(gone, 0, lens))
     graph.replay()
     torch.cuda.synchronize()
