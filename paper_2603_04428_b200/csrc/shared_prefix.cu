@@ -146,12 +146,19 @@ __device__ inline int inclusive_sum(int v) {
   }
   return v;
 }
-// The list is cut for n CTAs; a CTA's range begins at cut(), cta_of() is the CTA whose range holds position u.
+// The list is cut for n CTAs, the first total % n of them with a position more; a CTA's range begins at begin(), cta_of() is the CTA
+// whose range holds position u.
 struct Cut {
-  int total, n;
-  __device__ Cut(int total_, int grid) : total(total_), n(min(grid, max(1, total_))) {}
-  __device__ int begin(int c) const { return (int)((long long)total * c / n); }
-  __device__ int cta_of(int u) const { return (int)(((long long)(u + 1) * n - 1) / total); }
+  int n, each, more;
+  __device__ Cut(int total, int grid) : n(min(grid, max(1, total))) {
+    each = (int)((unsigned)total / (unsigned)n);
+    more = total - each * n;
+  }
+  __device__ int begin(int c) const { return c * each + min(c, more); }
+  __device__ int cta_of(int u) const {
+    const int big = more * (each + 1);
+    return u < big ? (int)((unsigned)u / (unsigned)(each + 1)) : more + (int)((unsigned)(u - big) / (unsigned)each);
+  }
 };
 
 // One CTA's part of a segment.  Records are named segment + CTA: both are in order, so no two parts share one.
@@ -301,7 +308,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           tiles = __shfl_sync(0xffffffffu, t, 31);
         }
       }
-      asm volatile("griddepcontrol.wait;" ::: "memory");
       int n = 0;                                         // segments handed out
       bool ok = true;
       auto hand_out = [&](const Segment& s) {
@@ -312,16 +318,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           mbar_arrive(&sm.info_full[n % kInfo]);
         }
       };
+      bool waited = false;
 #pragma unroll 1
       for (int gr = first; ok && any && start < u1; ++gr) {
         const Group q = group_of<kRows>(P, gr);
-        int lead = -1;                                   // the first agent that has the prefix
-#pragma unroll 1
-        for (int base = 0; base < q.n && lead < 0; base += 32) {
-          const int a = q.agent0 + base + lane, kv = base + lane < q.n ? P.kv_lens[a] : -1;
-          const unsigned has = __ballot_sync(0xffffffffu, kv >= q.prefix && kv > 0 && kv <= P.max_kv_len);
-          if (has) lead = q.agent0 + base + __ffs(has) - 1;
-        }
+        const int lead = first_holder(P.kv_lens, q.agent0, q.n, q.prefix, P.max_kv_len);             // the agent that the prefix is read through
         const int segments = q.tiles * y.Hkv;
         int k = q.cost > 0 && u0 > start ? (u0 - start) / q.cost : 0;
         if (lead < 0 || q.cost == 0) k = segments;
@@ -337,6 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           s.lead = lead; s.head = k - t * y.Hkv;
           s.prefix = q.prefix; s.step0 = from; s.steps = to - from; s.record = tile0 * y.Hkv + k + (int)blockIdx.x;
           hand_out(s);
+          if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+          waited = true;
           if (lane == 0) {
             const uint8_t* row = head_block(P.pool, y, P.layer, 0, s.head);
 #pragma unroll 1
@@ -363,6 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       }
       Segment last = {};
       hand_out(last);
+      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");        // or this grid could complete before the one it follows
       // a CTA that is giving up still lets its own copies land before shared memory is released
       if (lane == 0 && *abort_flag)
 #pragma unroll 1
@@ -434,6 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       // =============================== query rows =================================================
       constexpr int kLanes = D == 128 ? 16 : 32, kAtOnce = 4, kStride = 2 * (32 / kLanes);     // lanes of a row, rows in flight, rows of both warps
       asm volatile("griddepcontrol.wait;" ::: "memory");
+      const float per_rep = 1.f / (float)y.n_rep;
       const int piece = lane % kLanes, sub = (warp - kQueryWarp) * (32 / kLanes) + lane / kLanes;
 #pragma unroll 1
       for (int n = 0;; ++n) {
@@ -449,9 +454,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           uint4 v[kAtOnce];
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
-            const int r = base + kStride * u, a = (row0 + r) / y.n_rep;
+            const int r = base + kStride * u, row = row0 + r;
+            int a = (int)((float)row * per_rep);         // row / n_rep: the quotient of floats may be off by one
+            a -= a * y.n_rep > row;
+            a += (a + 1) * y.n_rep <= row;
             v[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows && piece < D / 8) v[u] = *reinterpret_cast<const uint4*>(q + ((size_t)a * y.Hq + (row0 + r - a * y.n_rep)) * D);
+            if (r < rows && piece < D / 8) v[u] = *reinterpret_cast<const uint4*>(q + ((size_t)a * y.Hq + (row - a * y.n_rep)) * D);
           }
 #pragma unroll
           for (int u = 0; u < kAtOnce; ++u) {
@@ -861,7 +869,7 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
     rec_ml += (size_t)record * ml_stride + 2 * row;
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int kQuads = Dv / 128;
+  constexpr int kQuads = Dv / 128, kAtOnce = 16 / kQuads;                  // parts whose numbers are asked for together with their weights
   float4 acc[kQuads];
   float M = -INFINITY, L = 0.f;
   bool bad = !fine || kv == 0;
@@ -876,25 +884,32 @@ __global__ void __launch_bounds__(128) shared_prefix_merge_kernel(const __grid_c
     bad = lse == -INFINITY;
   }
 #pragma unroll 1
-  for (int base = 0; base < parts; base += 32) {
-    const int n = min(32, parts - base);
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < n) ml = __ldcg(reinterpret_cast<const float2*>(rec_ml + (base + lane) * ml_stride));
+  for (int base = 0; base < parts; base += kAtOnce) {
+    const int n = min(kAtOnce, parts - base);
+    const float2 ml = lane < n ? __ldcg(reinterpret_cast<const float2*>(rec_ml + (base + lane) * ml_stride)) : make_float2(-INFINITY, 0.f);
+    float4 v[kAtOnce][kQuads];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+      if (j < n) {
+#pragma unroll
+        for (int k = 0; k < kQuads; ++k) v[j][k] = __ldcg(reinterpret_cast<const float4*>(rec + (base + j) * stride + 128 * k + 4 * lane));
+      }
     bad |= __any_sync(0xffffffffu, ml.y < 0.f) != 0;
-    const float* o = rec + base * stride + 4 * lane;
     const float m = fmaxf(M, warp_max(ml.x));
     const float keep = M == -INFINITY ? 0.f : fast_exp2(M - m), e = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
     L = L * keep + warp_sum(e * ml.y);
     M = m;
 #pragma unroll
     for (int k = 0; k < kQuads; ++k) { acc[k].x *= keep; acc[k].y *= keep; acc[k].z *= keep; acc[k].w *= keep; }
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) {
-      const float f = __shfl_sync(0xffffffffu, e, j);
 #pragma unroll
-      for (int k = 0; k < kQuads; ++k) {
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(o + j * stride + 128 * k));
-        acc[k].x = fmaf(f, v.x, acc[k].x); acc[k].y = fmaf(f, v.y, acc[k].y); acc[k].z = fmaf(f, v.z, acc[k].z); acc[k].w = fmaf(f, v.w, acc[k].w);
+    for (int j = 0; j < kAtOnce; ++j) {
+      const float f = __shfl_sync(0xffffffffu, e, j);
+      if (j < n) {
+#pragma unroll
+        for (int k = 0; k < kQuads; ++k) {
+          acc[k].x = fmaf(f, v[j][k].x, acc[k].x); acc[k].y = fmaf(f, v[j][k].y, acc[k].y);
+          acc[k].z = fmaf(f, v[j][k].z, acc[k].z); acc[k].w = fmaf(f, v[j][k].w, acc[k].w);
+        }
       }
     }
   }
