@@ -235,28 +235,33 @@ int q4kv_decode_attention_layers(const q4kv_spec* spec, void* pool, int32_t n_bl
                                  void* workspace, size_t workspace_bytes, int32_t* status_flags, void* stream);
 
 /* Decode attention for agents that share prefixes (forks of a common context, q4kv_allocator_fork): as q4kv_decode_attention,
- * with the keys and values of a group's prefix read and expanded once for all agents of the group.
+ * with the keys and values of a group's prefix read and expanded once for the agents of the group.  Where that would take longer
+ * than every agent reading its own -- few agents, short prefixes -- the call has each agent read its own, in one launch.
+ *   batch        as for the other calls: every agent's row lists all of its blocks, those of the prefix included
  *   group_offs   device int32 [n_groups + 1], ascending from 0 to n_agents: group g holds agents group_offs[g] .. group_offs[g+1] - 1
  *                (an agent that shares nothing is a group of its own; a group may be empty)
  *   prefix_lens  device int32 [n_groups]: the first prefix_lens[g] tokens of the group's agents are the same.  Any length: also one
  *                that ends inside a block, of which each agent then holds a copy (0: nothing is shared).  That they are the same is the
- *                caller's word: the prefix is read through the block-table row of the group's first agent with tokens, an agent's own
- *                tokens, positions prefix_lens[g] .. kv_len - 1, through its own row, whose entries for whole blocks of the prefix
- *                are not read.
+ *                caller's word: the prefix may be read through the row of any of the group's agents with tokens.
  *   n_groups     1 .. n_agents
  *   kv_lens      lengths with the prefix and the current token (append it first: q4kv_quantize_append).  kv_len == prefix_lens[g]
  *                is an agent without tokens of its own; kv_len == 0 gives zeros and lse = -inf without a flag.  A length below
  *                its group's prefix, negative or above max_kv_len, a bad prefix length, an agent outside every group, or offsets
  *                that do not ascend raise Q4KV_FLAG_BAD_LENGTH and give zeros for the agents concerned.
- *   workspace    at least q4kv_workspace_bytes_shared_prefix bytes.  Its first Q4KV_WORKSPACE_HEADER_BYTES are neither read nor
- *                written and nothing behind them carries over, so a workspace may also serve the other attention calls.
+ *   max_kv_len   as for q4kv_decode_attention; which way a call takes is estimated from it, n_agents and n_groups, so a bound near
+ *                the lengths serves best
+ *   workspace    at least q4kv_workspace_bytes_shared_prefix bytes, its header zeroed once as for q4kv_decode_attention, which may
+ *                share it
  * Like the other lengths, group_offs and prefix_lens are read before the preceding kernels of the stream have completed.
- * A bad block in the prefix gives zeros for every agent of its group, one among an agent's own blocks for that agent.  Sliding
- * windows have no argument here: their layers attend few keys each (q4kv_decode_attention).
- * Accuracy: that of the kernels that expand the cache into binary16 tiles.
- * Covered: d_qk = d_v = 128 with at most 64 query heads per KV head, d_qk = d_v = 256 and d_qk 192 / d_v 128 with at most 32; V not
- * aliasing K; exact_products == 0 and softmax_scale <= 2/sqrt(d_qk); at most 512 agents, and n_agents * n_kv_heads * max_kv_len
- * below 2^35.  Anything else returns Q4KV_EUNSUPPORTED and the caller makes the q4kv_decode_attention call. */
+ * A bad block gives zeros for every agent that reads it: one of the prefix for all the agents that read it through that row, one
+ * among an agent's own blocks for that agent.  Sliding windows have no argument here: their layers attend few keys each
+ * (q4kv_decode_attention).
+ * Accuracy: agents by themselves, and agents' own tokens, as q4kv_decode_attention.  Prefixes of groups: the scores are exact
+ * products with binary32 sums and each probability times a value's scale is rounded once to binary16; or, where
+ * softmax_scale <= 2/sqrt(d_qk) and many query rows share a prefix, the kernels that expand the cache into binary16 tiles.
+ * Covered: d_qk = d_v in {128, 256} and d_qk 192 / d_v 128, V not aliasing K, exact_products == 0, n_agents * n_kv_heads
+ * times the sets of 8 (d_qk = 128) or 4 query heads of a KV head at most 16384, and contexts whose work lists fit 32-bit numbers.
+ * Anything else returns Q4KV_EUNSUPPORTED and the caller makes the q4kv_decode_attention call. */
 size_t q4kv_workspace_bytes_shared_prefix(const q4kv_spec* spec, int32_t n_agents, int32_t max_kv_len, int32_t n_groups);
 int q4kv_shared_prefix_decode_attention(const q4kv_spec* spec, const void* pool, int32_t n_blocks, int32_t layer,
                                         const q4kv_batch* batch, const int32_t* kv_lens, int32_t max_kv_len,

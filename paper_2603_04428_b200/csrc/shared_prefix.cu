@@ -31,6 +31,8 @@
 //     ends the set's stores of P.
 // All waits are bounded; one that runs out raises Q4KV_FLAG_INTERNAL, lets the copies and the tensor pipe drain and gives the
 // tensor memory back.
+#include <cmath>
+
 #include "prefill_common.cuh"
 
 namespace q4kv {
@@ -939,11 +941,35 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 //   kAlone: every agent by itself, one launch of the decode kernel.  kList: the prefixes by the kernel above.  kTiles: by the prefill
 //   kernel, which expands a block once for 256 score rows (128 at d = 256 and 192 / 128) instead of unpacking it for 32.
 enum class Route { kAlone, kList, kTiles };
+// The way with the least estimated time, in us.  m: megabytes of keys and values at the longest length, which is all that is known here,
+// of one agent.  alone: a fixed part, m for every agent and every 8 (d = 128) or 4 query heads to a KV head, and the merge by output rows.
+// list: m for every group and every 32 score rows (16 at d = 256; 16 or fewer at the other dimensions cost three quarters).  tiles: m for
+// every group and every 256 score rows (128), at least the time of one CTA's run over the longest length.  Fitted to 330 measured cases
+// of 2 to 96 agents in 1 or 3 groups on 2000 to 32000 shared tokens with 200 of their own, 1 to 64 query heads to a KV head: the choice
+// costs 0.6 % over the best of the three on average, 22 % at most.  Measured alone / list / tiles, one group unless said otherwise:
+//   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  29.0      32 agents on 32000         206.4 / 99.4 / 55.6
+//   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  29.1      on 32000                    58.0 / 32.1 / 52.9
+//   8 KV heads of 8, d = 128, 16 agents in each of 3 on 8000  107.3 / 100.2 /  71.8      2 agents on 2000: alone in every shape
+//   8 KV heads of 2, d = 256, 16 agents on 32000              220.5 /  76.4 /  67.1      on 2000                     24.8 / 27.3 / 27.9
+//   16 KV heads of 1, d = 192 and 128, 32 agents on 8000      132.6 /  53.6 /  42.3      on 2000                     46.3 / 39.5 / 34.6
+struct RouteCost {
+  double alone[3], list[3], tiles[3];      // fixed, a megabyte, a thousand output rows
+};
 Route route_of(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool tiles_allowed) {
   if (n_groups >= n_agents) return Route::kAlone;        // nothing is shared
-  const long long rows = (long long)n_agents * y.n_rep / n_groups;           // of an average group and KV head
-  if (tiles_allowed && rows > 64 && (prefill_umma_supported(y) || prefill_umma_1tile_supported(y))) return Route::kTiles;
-  return Route::kList;
+  constexpr RouteCost k128 = {{7., .185, 3.}, {18., .54, 5.}, {20., .88, 5.}}, k192 = {{7., .165, 3.}, {20., .5, 12.}, {17., .61, 10.}},
+                      k256 = {{9., .18, 5.}, {23., .3, 9.}, {25., .52, 11.}};
+  const RouteCost& k = y.D == 128 ? k128 : y.D == 192 ? k192 : k256;
+  const double m = 1e-6 * y.chunk_bytes / kChunkTokens * y.Hkv * max_kv_len, all = 1e-3 * n_agents * y.Hq;
+  const double rows = (double)n_agents * y.n_rep / n_groups;             // of an average group and KV head
+  const double passes = y.D == 256 ? ceil(rows / 16.) : rows <= 16. ? 0.75 : ceil(rows / 32.);
+  const double alone = k.alone[0] + k.alone[1] * m * n_agents * ceil(y.n_rep / (y.D == 128 ? 8. : 4.)) + k.alone[2] * all;
+  const double list = k.list[0] + k.list[1] * m * n_groups * passes + k.list[2] * all;
+  const double tiles =
+      k.tiles[0] + fmax(k.tiles[1] * m * n_groups * ceil(rows / (y.D == 128 ? 256. : 128.)), 1e-3 * max_kv_len) + k.tiles[2] * all;
+  const bool may_tile = tiles_allowed && (prefill_umma_supported(y) || prefill_umma_1tile_supported(y));
+  if (alone <= list && !(may_tile && tiles < alone)) return Route::kAlone;
+  return may_tile && tiles < list ? Route::kTiles : Route::kList;
 }
 // The launch of the prefill kernel: groups take the agents' place
 int tile_queries(const Layout& y) { return prefill_umma_supported(y) ? 2 * (128 / y.n_rep) : 128 / y.n_rep; }
@@ -1021,13 +1047,12 @@ bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int 
          (2ll * n_agents * y.Hq / max_rows_of(y) + n_agents * y.Hkv) * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
 }
 
+// Whatever way a call takes: one workspace serves shorter contexts and any softmax scale.
 size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len) {
-  size_t most = 0;                                       // whatever the softmax scale
-  for (const bool tiles : {false, true}) {
-    const size_t end = sections_of(y, n_agents, n_groups, max_kv_len, route_of(y, n_agents, n_groups, max_kv_len, tiles)).end;
-    if (end > most) most = end;
-  }
-  return most;
+  const size_t list = sections_of(y, n_agents, n_groups, max_kv_len, Route::kList).end;
+  if (!prefill_umma_supported(y) && !prefill_umma_1tile_supported(y)) return list;
+  const size_t tiles = sections_of(y, n_agents, n_groups, max_kv_len, Route::kTiles).end;
+  return tiles > list ? tiles : list;
 }
 
 // workspace: with its header (the decode launch's arrival counters)
