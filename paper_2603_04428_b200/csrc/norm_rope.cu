@@ -23,7 +23,8 @@ constexpr int kThreads = 256;
 struct Params {
   q4kv_norm_rotation how;
   int d, hq, hk;              // hq or hk is 0 when that side is not asked for
-  int n_agents;
+  int rows, n_agents;
+  int parts, q_parts, part_heads;      // warps of a token, those of its query heads, heads of a warp
   const int32_t* pos;
   const int32_t* offs;
   const uint16_t* q;
@@ -52,12 +53,44 @@ __device__ inline uint4 pack8(const float (&x)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// kHeads: heads a thread works on at once (their loads are in flight together)
-template <int kLanes, int kVecs, int kHeads>
+__device__ inline void load8(const float* p, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+
+// A warp's work: heads [h_begin, h_end) of one token; kHeads: heads a lane works on at once (their loads are in flight together).
+// kFew: a launch of few tokens, whose angles are ready before the wait for the preceding kernel; else the first heads' loads are in
+// flight while the angles are computed.
+template <int kLanes, int kVecs, int kHeads, bool kFew>
 __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_constant__ Params P) {
-  extern __shared__ float2 turn[];                       // (cos, sin) * rot_scale
+  extern __shared__ __align__(16) float turns[];         // a warp's cosines * rot_scale, then its sines * rot_scale
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int row = blockIdx.x, lane = threadIdx.x & 31;
+  constexpr int kGroups = 32 / kLanes;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / kLanes, l = lane % kLanes;
+  const long long unit = (long long)blockIdx.x * (kThreads / 32) + warp;
+  const int row = (int)(unit / P.parts), part = (int)(unit % P.parts), pieces = P.d / 8;
+  if (row >= P.rows) return;                             // whole warps; no barrier of the block follows
+  const bool is_q = part < P.q_parts;
+  const int h_begin = (is_q ? part : part - P.q_parts) * P.part_heads, heads = is_q ? P.hq : P.hk, h_end = min(h_begin + P.part_heads, heads);
+  const uint16_t* in = is_q ? P.q + row * P.q_stride : P.k + row * P.k_stride;
+  uint16_t* out = is_q ? P.q_out + (size_t)row * heads * P.d : P.k_out + (size_t)row * heads * P.d;
+  const uint16_t* w = P.how.norm_dim > 0 ? (const uint16_t*)(is_q ? P.how.q_weight : P.how.k_weight) : nullptr;
+  uint4 v[kHeads][kVecs];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < kHeads; ++u) {
+      const int h = h0 + u * kGroups + group;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const int p = i * kLanes + l;
+        v[u][i] = h < h_end && p < pieces ? *reinterpret_cast<const uint4*>(in + h * P.d + 8 * p) : make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+  };
+  if (!kFew) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    load(h_begin);
+  }
   // the agent of the row: offsets at or below it
   int before = 0;
   for (int i = 0; i <= P.n_agents; i += 32) {
@@ -66,129 +99,166 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
     before += n;
     if (n < 32) break;
   }
-  if (before == 0 || before > P.n_agents) return;        // rows of no agent are left as they are (uniform in the CTA)
-  const int a = before - 1;
-  const int first = P.pos[a];
+  if (before == 0 || before > P.n_agents) return;        // rows of no agent are left as they are
+  const int first = P.pos[before - 1], ahead = row - P.offs[before - 1];
   const bool bad = first < 0;
-  if (bad && threadIdx.x == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
+  if (bad && lane == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
   const int half = P.how.rot_dim / 2;
-  const double position = (double)first + (double)(row - P.offs[a]);
-  for (int j = threadIdx.x; j < half; j += kThreads) {
+  float* cosine = turns + warp * P.how.rot_dim;
+  float* sine = cosine + half;
+  const double position = (double)first + (double)ahead;
+  for (int j = lane; j < half; j += 32) {
     const double t = position * (double)P.how.inv_freq[j] * 0.31830988618379067154;     // in half turns
     float s, c;
     sincospif((float)(t - 2.0 * rint(0.5 * t)), &s, &c);
-    turn[j] = make_float2(c * P.how.rot_scale, s * P.how.rot_scale);
+    cosine[j] = c * P.how.rot_scale;
+    sine[j] = s * P.how.rot_scale;
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int group = threadIdx.x / kLanes, l = threadIdx.x % kLanes, pieces = P.d / 8;
-  const uint16_t* in[kHeads];
-  uint4 v[kHeads][kVecs];
-#pragma unroll
-  for (int u = 0; u < kHeads; ++u) {
-    const int h = (blockIdx.y * kHeads + u) * (kThreads / kLanes) + group;
-    in[u] = h < P.hq ? P.q + row * P.q_stride + (size_t)h * P.d
-                     : h < P.hq + P.hk ? P.k + row * P.k_stride + (size_t)(h - P.hq) * P.d : nullptr;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int p = i * kLanes + l;
-      v[u][i] = in[u] && p < pieces && !bad ? *reinterpret_cast<const uint4*>(in[u] + 8 * p) : make_uint4(0u, 0u, 0u, 0u);
-    }
+  if (kFew) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    load(h_begin);
   }
-  __syncthreads();                                       // the angles
+  __syncwarp();
   const int rb = P.how.rot_begin / 8, re = rb + P.how.rot_dim / 8, apart = P.how.rot_dim / 16;     // in pieces
+  auto turned = [&](int p) { return p >= rb && p < re; };
+  auto mate = [&](int p) { return P.how.interleaved || !turned(p) ? p : p < rb + apart ? p + apart : p - apart; };
+  auto weight = [&](int p, float (&g)[8]) {
+    if (w && 8 * p < P.how.norm_dim) {
+      unpack8(*reinterpret_cast<const uint4*>(w + 8 * p), g);
 #pragma unroll
-  for (int u = 0; u < kHeads; ++u) {
-    const int h = (blockIdx.y * kHeads + u) * (kThreads / kLanes) + group;
-    const uint16_t* w = reinterpret_cast<const uint16_t*>(h < P.hq ? P.how.q_weight : P.how.k_weight);
-    float norm = 1.f;
-    if (P.how.norm_dim > 0) {                            // for every lane of a warp, whichever of its heads have a weight
-      float sum = 0.f;
+      for (int e = 0; e < 8; ++e) g[e] += P.how.weight_offset;
+    } else {
 #pragma unroll
-      for (int i = 0; i < kVecs; ++i) {
-        float x[8];
-        unpack8(v[u][i], x);
-        if (8 * (i * kLanes + l) < P.how.norm_dim) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
-        }
-      }
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o, kLanes);
-      norm = rsqrtf(sum / (float)P.how.norm_dim + P.how.eps);
+      for (int e = 0; e < 8; ++e) g[e] = 1.f;
     }
-    auto normed = [&](uint4 piece, int p, float (&x)[8]) {
-      unpack8(piece, x);
-      if (w && 8 * p < P.how.norm_dim) {
-        float g[8];
-        unpack8(*reinterpret_cast<const uint4*>(w + 8 * p), g);
+  };
+  // piece p of a normed and turned head is own * x + other * z, z being the other elements of its pairs
+  auto factors = [&](int p, float (&own)[8], float (&other)[8]) {
+    weight(p, own);
+    if (!turned(p)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * norm * (g[e] + P.how.weight_offset);
+      for (int e = 0; e < 8; ++e) other[e] = 0.f;
+    } else if (P.how.interleaved) {
+      const float4 c = *reinterpret_cast<const float4*>(cosine + 4 * (p - rb)), s = *reinterpret_cast<const float4*>(sine + 4 * (p - rb));
+      const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        other[2 * e] = -sn[e] * own[2 * e + 1];
+        other[2 * e + 1] = sn[e] * own[2 * e];
+        own[2 * e] *= cs[e];
+        own[2 * e + 1] *= cs[e];
       }
-    };
-    uint4 y[kVecs];
+    } else {
+      const bool low = p < rb + apart;
+      float c[8], s[8];
+      load8(cosine + 8 * ((low ? p : p - apart) - rb), c);
+      load8(sine + 8 * ((low ? p : p - apart) - rb), s);
+      weight(mate(p), other);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        own[e] *= c[e];
+        other[e] *= low ? -s[e] : s[e];
+      }
+    }
+  };
+  auto is_normed = [&](int p) { return w && 8 * p < P.how.norm_dim; };
+  float own[8], other[8];
+  if (kVecs == 1) factors(l, own, other);                // the same for all of the token's heads on this side
+  for (int h0 = h_begin;;) {
+    float norm[kHeads];
+#pragma unroll
+    for (int u = 0; u < kHeads; ++u) {
+      norm[u] = 1.f;
+      if (w) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          float x[8];
+          unpack8(v[u][i], x);
+          if (8 * (i * kLanes + l) < P.how.norm_dim) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+          }
+        }
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o, kLanes);
+        norm[u] = rsqrtf(sum / (float)P.how.norm_dim + P.how.eps);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int p = i * kLanes + l;
-      float x[8];
-      normed(v[u][i], p, x);
-      const bool turned = p >= rb && p < re;
-      if (P.how.interleaved) {
-        if (turned) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 t = turn[4 * (p - rb) + e];
-            const float x0 = x[2 * e], x1 = x[2 * e + 1];
-            x[2 * e] = x0 * t.x - x1 * t.y;
-            x[2 * e + 1] = x1 * t.x + x0 * t.y;
-          }
-        }
-      } else {
-        const bool low = p < rb + apart;
-        const int q = turned ? (low ? p + apart : p - apart) : p;
-        float z[8];
-        if (kVecs == 1) {                                // every lane takes part
-#pragma unroll
-          for (int e = 0; e < 8; ++e) z[e] = __shfl_sync(0xffffffffu, x[e], q, kLanes);
-        } else if (turned && in[u] && !bad) {
-          normed(*reinterpret_cast<const uint4*>(in[u] + 8 * q), q, z);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) z[e] = 0.f;
-        }
-        if (turned) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 t = turn[8 * ((low ? p : q) - rb) + e];
-            x[e] = low ? x[e] * t.x - z[e] * t.y : x[e] * t.x + z[e] * t.y;
-          }
-        }
+      const int p = i * kLanes + l, q = mate(p);
+      if (kVecs > 1) {
+        if (p >= pieces || (!turned(p) && !is_normed(p))) continue;
+        factors(p, own, other);
       }
-      y[i] = pack8(x);
+#pragma unroll
+      for (int u = 0; u < kHeads; ++u) {
+        uint4 mates = v[u][i];
+        if (!P.how.interleaved) {
+          if (kVecs == 1) {                              // every lane takes part
+            mates.x = __shfl_sync(0xffffffffu, mates.x, q, kLanes);
+            mates.y = __shfl_sync(0xffffffffu, mates.y, q, kLanes);
+            mates.z = __shfl_sync(0xffffffffu, mates.z, q, kLanes);
+            mates.w = __shfl_sync(0xffffffffu, mates.w, q, kLanes);
+          } else if (h0 + u * kGroups + group < h_end) {
+            mates = *reinterpret_cast<const uint4*>(in + (h0 + u * kGroups + group) * P.d + 8 * q);
+          }
+        }
+        float x[8], z[8];
+        unpack8(v[u][i], x);
+        unpack8(mates, z);
+        const float nx = is_normed(p) ? norm[u] : 1.f, nz = is_normed(q) ? norm[u] : 1.f;
+        const bool t = turned(p);
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float m = t ? (P.how.interleaved ? z[e ^ 1] : z[e]) : 0.f;       // what it is not paired with, it does not see
+          y[e] = fmaf(m * nz, other[e], x[e] * nx * own[e]);
+        }
+        v[u][i] = pack8(y);
+      }
     }
     if (kVecs > 1) __syncwarp();                         // rows that go back where they came from: all reads come first
-    uint16_t* out = h < P.hq ? P.q_out + ((size_t)row * P.hq + h) * P.d : P.k_out + ((size_t)row * P.hk + (h - P.hq)) * P.d;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int p = i * kLanes + l;
-      if (in[u] && p < pieces) *reinterpret_cast<uint4*>(out + 8 * p) = bad ? make_uint4(0u, 0u, 0u, 0u) : y[i];
+    for (int u = 0; u < kHeads; ++u) {
+      const int h = h0 + u * kGroups + group;
+#pragma unroll
+      for (int i = 0; i < kVecs; ++i) {
+        const int p = i * kLanes + l;
+        if (h < h_end && p < pieces) *reinterpret_cast<uint4*>(out + h * P.d + 8 * p) = bad ? make_uint4(0u, 0u, 0u, 0u) : v[u][i];
+      }
     }
+    h0 += kHeads * kGroups;
+    if (h0 >= h_end) break;
+    load(h0);
   }
 }
 
-template <int kLanes, int kVecs, int kHeads>
-cudaError_t launch(const Params& P, int rows, cudaStream_t st) {
-  const int per_cta = kThreads / kLanes * kHeads;
+// part_heads: heads of a warp
+template <int kLanes, int kVecs, int kHeads, bool kFew>
+cudaError_t launch(Params P, int part_heads, cudaStream_t st) {
+  P.part_heads = part_heads;
+  P.q_parts = (P.hq + part_heads - 1) / part_heads;
+  P.parts = P.q_parts + (P.hk + part_heads - 1) / part_heads;
+  constexpr int warps = kThreads / 32;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(rows, (P.hq + P.hk + per_cta - 1) / per_cta);
+  cfg.gridDim = dim3((unsigned)(((long long)P.rows * P.parts + warps - 1) / warps));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(float2) * (size_t)(P.how.rot_dim / 2);
+  cfg.dynamicSmemBytes = sizeof(float) * (size_t)P.how.rot_dim * warps;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, norm_rope_kernel<kLanes, kVecs, kHeads>, P);
+  return cudaLaunchKernelEx(&cfg, norm_rope_kernel<kLanes, kVecs, kHeads, kFew>, P);
+}
+template <int kLanes, int kVecs, int kHeads>
+cudaError_t launch(const Params& P, cudaStream_t st) {
+  constexpr int at_once = 32 / kLanes;
+  if (P.rows < 4 * sm_count()) return launch<kLanes, kVecs, 1, true>(P, at_once, st);
+  return launch<kLanes, kVecs, kHeads, false>(P, at_once * kHeads * 2, st);
 }
 
 }  // namespace
@@ -198,17 +268,16 @@ cudaError_t launch_norm_rope(const Layout& y, const q4kv_norm_rotation& how, int
                              int32_t* flags, cudaStream_t st) {
   Params P;
   P.how = how;
-  P.d = y.D; P.hq = q ? y.Hq : 0; P.hk = k ? y.Hkv : 0; P.n_agents = n_agents; P.pos = pos; P.offs = offs;
+  P.d = y.D; P.hq = q ? y.Hq : 0; P.hk = k ? y.Hkv : 0; P.rows = rows; P.n_agents = n_agents; P.pos = pos; P.offs = offs;
   P.q = (const uint16_t*)q; P.k = (const uint16_t*)k; P.q_stride = q_stride; P.k_stride = k_stride;
   P.q_out = (uint16_t*)q_out; P.k_out = (uint16_t*)k_out; P.flags = flags;
-  const bool few = rows < 4 * sm_count();                // few tokens: more CTAs, each with fewer heads
-  if (y.D == 64) return few ? launch<8, 1, 1>(P, rows, st) : launch<8, 1, 4>(P, rows, st);
-  if (y.D == 128) return few ? launch<16, 1, 1>(P, rows, st) : launch<16, 1, 4>(P, rows, st);
-  if (y.D == 192) return few ? launch<8, 3, 1>(P, rows, st) : launch<8, 3, 2>(P, rows, st);
-  if (y.D <= 256) return few ? launch<32, 1, 1>(P, rows, st) : launch<32, 1, 4>(P, rows, st);
-  if (y.D <= 512) return launch<32, 2, 1>(P, rows, st);
-  if (y.D <= 768) return launch<32, 3, 1>(P, rows, st);
-  return launch<32, 4, 1>(P, rows, st);
+  if (y.D == 64) return launch<8, 1, 4>(P, st);
+  if (y.D == 128) return launch<16, 1, 4>(P, st);
+  if (y.D == 192) return launch<8, 3, 2>(P, st);
+  if (y.D <= 256) return launch<32, 1, 4>(P, st);
+  if (y.D <= 512) return launch<32, 2, 2>(P, st);
+  if (y.D <= 768) return launch<32, 3, 1>(P, st);
+  return launch<32, 4, 1>(P, st);
 }
 
 }  // namespace q4kv
