@@ -366,6 +366,7 @@ int q4kv_norm_rope(const q4kv_spec* spec, const q4kv_norm_rotation* how, int32_t
   if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(how->q_weight) ||
       !aligned16(how->k_weight))
     return Q4KV_EINVAL;
+  if ((int64_t)spec->n_q_heads + spec->n_kv_heads > 65535) return Q4KV_EUNSUPPORTED;     // grid limit
   const int64_t q_row = (int64_t)spec->n_q_heads * d, k_row = (int64_t)spec->n_kv_heads * d;
   constexpr int64_t kMost = INT64_MAX / 4 / INT32_MAX;     // byte offsets of every row stay within 63 bits
   if ((q && (q_stride < q_row || q_stride % 8 || q_stride > kMost)) || (k && (k_stride < k_row || k_stride % 8 || k_stride > kMost)))

@@ -118,6 +118,59 @@ def test_many_rows_and_few_give_the_same_bits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("case", CASES)
+def test_a_warp_that_takes_whole_tokens_gives_the_same_bits(case):
+    """Enough rows that a warp has a token's query and key heads, out of place and in place, against calls of few rows."""
+    hq, hkv, d, norm, offset, rot_begin, rot_dim, inter, scale = case
+    hq, hkv, n = 2 * hkv + 1 if hq > 2 * hkv else hq, hkv, 15001
+    if hq % hkv:
+        hq = hkv
+    f = theta(rot_dim)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((n, hq + hkv, d), device="cuda", generator=g).to(torch.bfloat16)
+    w = torch.randn((2, max(norm, 8)), device="cuda", generator=g).to(torch.bfloat16)
+    how = B.NormRotation.make(norm_dim=norm, q_weight=w[0] if norm else None, k_weight=w[1] if norm else None, weight_offset=offset,
+                              rot_begin=rot_begin, rot_dim=rot_dim, interleaved=inter, rot_scale=scale,
+                              inv_freq=None if f is None else torch.from_numpy(f).cuda())
+    spec = B.Spec.make(1, hq, hkv, d, min(d, 512))
+    q, k = x[:, :hq], x[:, hq:]
+    qo, ko, q1, k1 = (torch.empty((n, h, d), dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hq, hkv))
+    dev = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    B.q4kv_norm_rope(spec, how, 2, dev(5, 100), dev(0, 7000, n), n, q, k, qo, ko)
+    for lo in range(0, n, 500):
+        hi = min(lo + 500, n)
+        B.q4kv_norm_rope(spec, how, 2, dev(5 + lo, 100 + max(lo - 7000, 0)), dev(0, min(max(7000 - lo, 0), hi - lo), hi - lo), hi - lo,
+                         q[lo:hi], k[lo:hi], q1[lo:hi], k1[lo:hi])
+    assert torch.equal(qo, q1) and torch.equal(ko, k1)
+    q, k = q.contiguous(), k.contiguous()
+    B.q4kv_norm_rope(spec, how, 2, dev(5, 100), dev(0, 7000, n), n, q, k, q, k)
+    assert torch.equal(q, q1) and torch.equal(k, k1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [3, 900])
+@pytest.mark.parametrize("d, begin, dim, inter", [(128, 32, 64, False), (128, 32, 64, True), (192, 128, 64, True), (256, 0, 256, False),
+                                                  (512, 256, 64, False)])
+def test_elements_that_are_not_finite_reach_their_pair_alone(d, begin, dim, inter, rows):
+    f = torch.from_numpy(theta(dim)).cuda()
+    how = B.NormRotation.make(rot_begin=begin, rot_dim=dim, interleaved=inter, inv_freq=f)
+    spec = B.Spec.make(1, 2, 2, d, min(d, 256))
+    x = torch.randn((rows, 2, d), device="cuda").to(torch.bfloat16)
+    out, again = torch.empty_like(x), torch.empty_like(x)
+    offs, pos = torch.tensor([0, rows], dtype=torch.int32, device="cuda"), torch.tensor([9], dtype=torch.int32, device="cuda")
+    B.q4kv_norm_rope(spec, how, 1, pos, offs, rows, x, None, out, None)
+    for at, value in ((begin + 3, float("inf")), (begin + dim - 1, float("nan")), (d - 1, float("inf")), (0, float("nan"))):
+        y = x.clone()
+        y[1, 1, at] = value
+        B.q4kv_norm_rope(spec, how, 1, pos, offs, rows, y, None, again, None)
+        j = at - begin
+        mates = {at} if not 0 <= j < dim else {at, begin + (j ^ 1 if inter else (j + dim // 2) % dim)}
+        hit = torch.zeros_like(x, dtype=torch.bool)
+        hit[1, 1, list(mates)] = True
+        assert not torch.isfinite(again[hit]).any() and torch.equal(again[~hit], out[~hit])
+
+
+@pytest.mark.gpu
 def test_a_weight_for_one_side_leaves_the_other_without_norm():
     hq, hkv, d = 3, 1, 64                                # a warp holds query and key heads
     x = torch.randn((4, hq + hkv, d), device="cuda").to(torch.bfloat16)
@@ -171,7 +224,7 @@ def test_refusals():
                 dict(ko=0x200000, ks=264)):
         assert call(**bad) == B.EINVAL, bad
     for bad in (dict(norm_dim=12), dict(rot_dim=24), dict(rot_begin=4, rot_dim=64), dict(rot_dim=12, interleaved=1),
-                dict(sp=B.Spec.make(1, 8, 2, 96, 128))):
+                dict(sp=B.Spec.make(1, 8, 2, 96, 128)), dict(sp=B.Spec.make(1, 65535, 1, 128, 128))):
         assert call(**bad) == B.EUNSUPPORTED, bad
     assert call(total=0) == call(agents=0) == call(q=None, qo=None, k=None, ko=None) == B.OK
 
