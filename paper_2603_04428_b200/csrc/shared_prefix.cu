@@ -941,40 +941,55 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 //   kAlone: every agent by itself, one launch of the decode kernel.  kList: the prefixes by the kernel above.  kTiles: by the prefill
 //   kernel, which expands a block once for 256 score rows (128 at d = 256 and 192 / 128) instead of unpacking it for 32.
 enum class Route { kAlone, kList, kTiles };
+// The launch of the prefill kernel: groups take the agents' place.  Its keys are cut into parts; the unit of time is a 64-key block of
+// a tile, 1.3 us.  A CTA's start and end take four of them, and every part adds its records to what the merge reads, at 4 TB/s.
+// 64 agents of 32 / 8 heads on 32768 tokens: 18 parts, 144 CTAs (with the 9 of an ordinary prefill call's plan, which allows for ragged
+// tiles and stops at 16, 115 us a call instead of 88); 32 of 64 / 1 heads on 32000: 41.8 us instead of 56.4.
+constexpr int kMaxTileSplits = 128;
+struct TilePlan { int splits; double units; };
+int tile_queries(const Layout& y) { return prefill_umma_supported(y) ? 2 * (128 / y.n_rep) : 128 / y.n_rep; }
+TilePlan plan_tiles(const Layout& y, int n_agents, int n_groups, int max_kv_len, size_t bytes) {
+  const long long sms = sm_count();
+  const long long ctas = (n_groups + (long long)(n_agents - n_groups) / tile_queries(y)) * y.Hkv;     // at most, however groups are cut
+  const double blocks = max_kv_len / 64 + 1, merge = 1e-6 * prefill_record_bytes(y, n_agents, 1) / (4. * 1.3);
+  TilePlan best = {1, 1e30};
+  for (int s = 1; s <= kMaxTileSplits; ++s) {
+    // the kernel numbers blocks times parts in 32 bits
+    if (s > 1 && (s * 4 > blocks || (s + 1) * blocks > 2147483647. || prefill_record_bytes(y, n_agents, s) > bytes)) break;
+    const double t = (double)((ctas * s + sms - 1) / sms) * (blocks / s + 4.) + s * merge;
+    if (t < 0.97 * best.units) best = {s, t};
+  }
+  return best;
+}
+
 // The way with the least estimated time, in us.  m: megabytes of keys and values at the longest length, which is all that is known here,
 // of one agent.  alone: a fixed part, m for every agent and every 8 (d = 128) or 4 query heads to a KV head, and the merge by output rows.
-// list: m for every group and every 32 score rows (16 at d = 256; 16 or fewer at the other dimensions cost three quarters).  tiles: m for
-// every group and every 256 score rows (128), at least the time of one CTA's run over the longest length.  Fitted to 330 measured cases
-// of 2 to 96 agents in 1 or 3 groups on 2000 to 32000 shared tokens with 200 of their own, 1 to 64 query heads to a KV head: the choice
-// costs 0.6 % over the best of the three on average, 22 % at most.  Measured alone / list / tiles, one group unless said otherwise:
-//   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  29.0      32 agents on 32000         206.4 / 99.4 / 55.6
-//   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  29.1      on 32000                    58.0 / 32.1 / 52.9
+// list: m for every group and every 32 score rows (16 at d = 256; 16 or fewer at the other dimensions cost three quarters).  tiles: the
+// plan's units.  Fitted to 330 measured cases of 2 to 96 agents in 1 or 3 groups on 2000 to 32000 shared tokens with 200 of their own, 1
+// to 64 query heads to a KV head: the choice costs 0.4 % over the best of the three on average, 26 % at most.  Measured alone / list /
+// tiles, one group unless said otherwise:
+//   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  27.4      32 agents on 32000         206.4 / 99.4 / 52.2
+//   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  27.4      on 32000                    58.0 / 32.1 / 49.5
 //   8 KV heads of 8, d = 128, 16 agents in each of 3 on 8000  107.3 / 100.2 /  71.8      2 agents on 2000: alone in every shape
-//   8 KV heads of 2, d = 256, 16 agents on 32000              220.5 /  76.4 /  67.1      on 2000                     24.8 / 27.3 / 27.9
-//   16 KV heads of 1, d = 192 and 128, 32 agents on 8000      132.6 /  53.6 /  42.3      on 2000                     46.3 / 39.5 / 34.6
+//   8 KV heads of 2, d = 256, 16 agents on 32000              220.5 /  76.4 /  64.9      on 2000                     24.8 / 27.3 / 28.6
+//   16 KV heads of 1, d = 192 and 128, 32 agents on 8000      132.6 /  53.6 /  42.2      on 2000                     46.3 / 39.5 / 34.7
 struct RouteCost {
-  double alone[3], list[3], tiles[3];      // fixed, a megabyte, a thousand output rows
+  double alone[3], list[3], tiles[3];      // fixed, a megabyte (tiles: a unit), a thousand output rows
 };
 Route route_of(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool tiles_allowed) {
   if (n_groups >= n_agents) return Route::kAlone;        // nothing is shared
-  constexpr RouteCost k128 = {{7., .185, 3.}, {18., .54, 5.}, {20., .88, 5.}}, k192 = {{7., .165, 3.}, {20., .5, 12.}, {17., .61, 10.}},
-                      k256 = {{9., .18, 5.}, {23., .3, 9.}, {25., .52, 11.}};
+  constexpr RouteCost k128 = {{7., .185, 3.}, {18., .54, 5.}, {12., 1.14, 4.}}, k192 = {{7., .165, 3.}, {20., .5, 12.}, {12., .96, 7.}},
+                      k256 = {{9., .18, 5.}, {23., .3, 9.}, {17.4, 1.25, 8.3}};
   const RouteCost& k = y.D == 128 ? k128 : y.D == 192 ? k192 : k256;
   const double m = 1e-6 * y.chunk_bytes / kChunkTokens * y.Hkv * max_kv_len, all = 1e-3 * n_agents * y.Hq;
   const double rows = (double)n_agents * y.n_rep / n_groups;             // of an average group and KV head
   const double passes = y.D == 256 ? ceil(rows / 16.) : rows <= 16. ? 0.75 : ceil(rows / 32.);
   const double alone = k.alone[0] + k.alone[1] * m * n_agents * ceil(y.n_rep / (y.D == 128 ? 8. : 4.)) + k.alone[2] * all;
   const double list = k.list[0] + k.list[1] * m * n_groups * passes + k.list[2] * all;
-  const double tiles =
-      k.tiles[0] + fmax(k.tiles[1] * m * n_groups * ceil(rows / (y.D == 128 ? 256. : 128.)), 1e-3 * max_kv_len) + k.tiles[2] * all;
   const bool may_tile = tiles_allowed && (prefill_umma_supported(y) || prefill_umma_1tile_supported(y));
-  if (alone <= list && !(may_tile && tiles < alone)) return Route::kAlone;
-  return may_tile && tiles < list ? Route::kTiles : Route::kList;
-}
-// The launch of the prefill kernel: groups take the agents' place
-int tile_queries(const Layout& y) { return prefill_umma_supported(y) ? 2 * (128 / y.n_rep) : 128 / y.n_rep; }
-int tile_splits(const Layout& y, int n_agents, int n_groups, int max_kv_len, size_t bytes) {
-  return plan_prefill_splits(y, tile_queries(y), 1, n_groups, n_agents, (n_agents + n_groups - 1) / n_groups, max_kv_len, 0, bytes);
+  const double tiles =
+      may_tile ? k.tiles[0] + k.tiles[1] * plan_tiles(y, n_agents, n_groups, max_kv_len, (size_t)-1).units + k.tiles[2] * all : 1e30;
+  return alone <= list && alone <= tiles ? Route::kAlone : tiles < list ? Route::kTiles : Route::kList;
 }
 
 // The workspace behind the header: the decode launch's records, what it leaves for the agents' own tokens, the prefixes' records (a CTA
@@ -990,7 +1005,7 @@ Sections sections_of(const Layout& y, int n_agents, int n_groups, int max_kv_len
     s.rec_ml = s.rec_o = s.end = s.own_lse;
   } else if (route == Route::kTiles) {
     s.rec_o = s.rec_ml;
-    s.end = s.rec_o + align256(prefill_record_bytes(y, n_agents, tile_splits(y, n_agents, n_groups, max_kv_len, (size_t)-1)));
+    s.end = s.rec_o + align256(prefill_record_bytes(y, n_agents, plan_tiles(y, n_agents, n_groups, max_kv_len, (size_t)-1).splits));
   } else {
     const int rows = max_rows_of(y);
     const size_t tiles = q_rows / y.Hkv / rows + n_groups, records = tiles * y.Hkv + sm_count();
@@ -1078,7 +1093,7 @@ cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks
   cudaError_t e;
   if (route == Route::kTiles) {
     PrefillExtra x = {};
-    P.splits = x.n_splits = tile_splits(y, b.n_agents, n_groups, max_kv_len, workspace_bytes - kWorkspaceHeaderBytes - s.rec_o);
+    P.splits = x.n_splits = plan_tiles(y, b.n_agents, n_groups, max_kv_len, workspace_bytes - kWorkspaceHeaderBytes - s.rec_o).splits;
     x.records = P.rec_o; x.agent_lens = kv_lens; x.n_agents = b.n_agents; x.max_kv_len = max_kv_len;
     const q4kv_batch groups = {n_groups, b.max_blocks, b.block_tables};
     const auto launch = prefill_umma_supported(y) ? launch_prefill_umma : launch_prefill_umma_1tile;
