@@ -409,7 +409,8 @@ int q4kv_restore(const q4kv_spec* spec, const void* host_packed, size_t packed_b
 
 /* Copy blocks, layers layer_begin .. layer_begin + layer_count - 1, within a pool or from one pool to another of the same spec
  * (the device half of q4kv_allocator_fork, _truncate and _compact; also for moving into a pool of another size).
- *   copies   device int32 [n_copies][3]: source block in src_pool, destination block in dst_pool, tokens (0 .. 256)
+ *   copies   device int32 [n_copies][3]: source block in src_pool, destination block in dst_pool, tokens (0 .. 256); read, like the
+ *            lengths of the other calls, before the preceding kernels of the stream have completed
  * The 32-token chunks that hold the first `tokens` tokens of the block are copied whole, for every KV head; the rest of the
  * destination is left as it was.  In one call no destination may be named twice, and within one pool no block may be both a
  * source and a destination (which of the two contents a byte then gets is not defined); a block copied to itself stays as it is.

@@ -24,9 +24,11 @@ copy_blocks_kernel(uint32_t chunk_bytes, int heads, const uint8_t* src, int src_
   const bool bad_block = from < 0 || from >= src_blocks || to < 0 || to >= dst_blocks, bad_length = n < 0 || n > kBlockTokens;
   if (bad_block || bad_length) {
     if (threadIdx.x == 0) raise_flag(flags, (bad_block ? Q4KV_FLAG_BAD_BLOCK : 0) | (bad_length ? Q4KV_FLAG_BAD_LENGTH : 0));
+  }
+  if (bad_block || bad_length || warp * kChunkTokens >= n || (from == to && src == dst)) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // or a grid without copies could complete before the one it follows
     return;
   }
-  if (warp * kChunkTokens >= n || (from == to && src == dst)) return;
   const size_t chunk = (size_t)hk * kChunksPerBlock + warp, per_block = (size_t)heads * kChunksPerBlock;
   const uint4* a = reinterpret_cast<const uint4*>(src + (((size_t)layer * src_blocks + from) * per_block + chunk) * chunk_bytes);
   uint4* b = reinterpret_cast<uint4*>(dst + (((size_t)layer * dst_blocks + to) * per_block + chunk) * chunk_bytes);

@@ -103,7 +103,10 @@ __global__ void __launch_bounds__(kThreads, kFew ? 1 : ctas_of(kVecs)) norm_rope
   constexpr int kGroups = 32 / kLanes, kStep = kGroups * kHeads, kEarly = 4;
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, group = lane / kLanes, l = lane % kLanes;
   const int row = blockIdx.x * (kThreads / 32) + warp, part = blockIdx.y, d = kWhole ? 16 * kLanes : P.d, pieces = d / 8;
-  if (row >= P.rows) return;                             // whole warps; no barrier of the block follows
+  if (row >= P.rows) {                                   // whole warps; no barrier of the block follows
+    asm volatile("griddepcontrol.wait;" ::: "memory");   // or this grid could complete before the one it follows
+    return;
+  }
   const int h_begin = part * P.part_heads, h_last = min(h_begin + P.part_heads, P.hq + P.hk);
   // one side at a time: its heads [h, h_end) of in and out
   const uint16_t* in;
@@ -153,7 +156,10 @@ __global__ void __launch_bounds__(kThreads, kFew ? 1 : ctas_of(kVecs)) norm_rope
     }
     if (n < 32) break;
   }
-  if (before == 0 || before > P.n_agents) return;        // rows of no agent are left as they are
+  if (before == 0 || before > P.n_agents) {              // rows of no agent are left as they are
+    if (kFew) asm volatile("griddepcontrol.wait;" ::: "memory");
+    return;
+  }
   const int ahead = row - start;
   const bool bad = first < 0;
   if (bad && lane == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);

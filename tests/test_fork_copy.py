@@ -277,3 +277,41 @@ def test_forked_agents_hold_what_they_would_have_built_alone():
     for agent, n in ((0, 800), (1, 950)):
         assert torch.equal(cache.pack(agent, n), alone.pack(agent, n))
     assert cache.read_flags() == alone.read_flags() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("between", ["no tokens", "bad blocks", "onto themselves", "rows of no agent", "agents of no group"])
+def test_a_call_without_work_does_not_let_its_successor_overtake_its_predecessor(between):
+    """Copy, a call that has nothing to do, a copy of what the first one wrote: launches that overlap in a stream have to wait for
+    their predecessors also when they do nothing."""
+    n = 1500
+    spec, a, _ = _pool((2, 32, 8, 128, 128, False), n, 5)
+    b, c = torch.zeros_like(a), torch.zeros_like(a)
+    every = torch.tensor([(i, i, 256) for i in range(n)], dtype=torch.int32, device="cuda")
+    last = torch.tensor([(i, i, 256) for i in range(n - 40, n)], dtype=torch.int32, device="cuda")
+    none = {"no tokens": (0, 1, 0), "bad blocks": (-1, 0, 256), "onto themselves": (3, 3, 256)}.get(between)
+    x = torch.zeros((4, 32, 128), dtype=torch.bfloat16, device="cuda")
+    zeros = torch.zeros(256, dtype=torch.int32, device="cuda")
+    if none:
+        idle = torch.tensor([none] * 8, dtype=torch.int32, device="cuda")
+        call = lambda: B.q4kv_copy_blocks(spec, a, n, a, n, 0, 2, idle, 8)
+    elif between == "rows of no agent":
+        f = torch.ones(64, device="cuda")
+        how = B.NormRotation.make(rot_dim=128, inv_freq=f)
+        call = lambda: B.q4kv_norm_rope(spec, how, 2, zeros, zeros, 4, x, None, x, None)
+    else:
+        q = torch.zeros((200, 32, 128), dtype=torch.bfloat16, device="cuda")
+        out = torch.zeros_like(q)
+        tables = torch.zeros((200, 64), dtype=torch.int32, device="cuda")
+        bt = B.Batch(200, 64, tables.data_ptr())
+        ws = torch.zeros(B.q4kv_workspace_bytes_shared_prefix(spec, 200, 64 * 256, 1), dtype=torch.uint8, device="cuda")
+        call = lambda: B.q4kv_shared_prefix_decode_attention(spec, a, n, 0, bt, zeros, 64 * 256, zeros, zeros, 1, q, 0.1, out, B.OUT_BF16,
+                                                             None, ws)
+    for _ in range(10):
+        b.zero_()
+        c.zero_()
+        B.q4kv_copy_blocks(spec, a, n, b, n, 0, 2, every, n)
+        call()
+        B.q4kv_copy_blocks(spec, b, n, c, n, 0, 2, last, 40)
+        got, want = (t.view(2, n, 8, 8, -1)[:, n - 40:] for t in (c, a))
+        assert torch.equal(got, want)
