@@ -63,6 +63,7 @@ class NormRotation(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("norm_dim", "rot_begin", "rot_dim", "interleaved")] + \
                [(n, ctypes.c_float) for n in ("eps", "weight_offset", "rot_scale")] + [("reserved", ctypes.c_int32)] + \
                [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "inv_freq")]
+    device = None                # of its tensors
 
     @classmethod
     def make(cls, norm_dim=0, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0, rot_begin=0, rot_dim=0,
@@ -73,6 +74,9 @@ class NormRotation(ctypes.Structure):
         how = cls(norm_dim, rot_begin, rot_dim, int(bool(interleaved)), eps, weight_offset, rot_scale, 0, _ptr(q_weight),
                   _ptr(k_weight), _ptr(inv_freq))
         how.tensors = (q_weight, k_weight, inv_freq)
+        devices = {t.get_device() for t in how.tensors if t is not None}
+        assert len(devices) <= 1, "weights and frequencies of one device"
+        how.device = devices.pop() if devices else None
         return how
 
 
@@ -295,6 +299,7 @@ def q4kv_shared_prefix_decode_attention(spec, pool, n_blocks, layer, bt: Batch, 
 def q4kv_norm_rope(spec, how: NormRotation, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags=None):
     """Norm and rotation of the new query and key rows.  q, k: bfloat16 [total_new][heads][d_qk] whose first stride is free (a
     view of a fused projection); q_out, k_out contiguous, or the input itself."""
+    assert how.device is None or how.device == _device(), "a tensor lies on another device than the current one"
     _check(_native().norm_rope(spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, _stream(),
                                _device()), "q4kv_norm_rope")
 

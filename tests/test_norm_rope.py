@@ -263,3 +263,14 @@ def test_tensors_of_another_device_are_refused():
     assert call.norm_rope(spec, how, 1, 0x1000, 0x1000, 0, t, None, 0x2000, None, None, None, 1) == B.OK
     with pytest.raises(AssertionError, match="rows are"):
         call.norm_rope(spec, how, 1, 0x1000, 0x1000, 5, t, None, 0x2000, None, None, None, 1)
+    how.device = 1                                       # of its weights and frequencies
+    with pytest.raises(AssertionError, match="another device"):
+        _call_on(0, spec, how)
+
+
+def _call_on(device, spec, how):
+    keep, B._device = B._device, lambda: device
+    try:
+        B.q4kv_norm_rope(spec, how, 1, 0x1000, 0x1000, 0, None, None, None, None)
+    finally:
+        B._device = keep

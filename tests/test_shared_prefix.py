@@ -283,6 +283,41 @@ def test_bad_blocks_spoil_the_agents_that_read_them(wide, more):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("scale", [-1.0, -0.05, 0.0, 3.0])
+@pytest.mark.parametrize("shape, more", [((8, 2, 128, 128), 4), ((2, 2, 192, 128), 4), ((4, 2, 256, 256), 80)])
+def test_any_softmax_scale(shape, more, scale):
+    f = Forked(shape, [(600, [20, 300] + [1] * more), (300, [9, 0])], seed=41, wide=WIDE)
+    q = f.q()
+    out, lse = f.run(q, scale)
+    close(out, lse, *f.want(q, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("wide, more", [(1, 0), (WIDE, 4), (WIDE, 60)])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (2, 2, 192, 128), (4, 2, 256, 256)])
+def test_blocks_beyond_four_gigabytes(shape, wide, more):
+    """The same blocks, moved to the end of a pool of 9 GB and to its last layer: the same bits."""
+    from paper_2603_04428_b200 import harness as H
+    f = Forked(shape, [(700, [20, 300] + [1] * more), (300, [9, 0])], seed=40, wide=wide)
+    q, scale = f.q(), 1.0 / math.sqrt(shape[2])
+    out, lse = f.run(q, scale)
+    layers = 6
+    spec = B.Spec.make(layers, *shape)
+    one = B.q4kv_pool_bytes(spec, 1)
+    n = (9 << 30) // one
+    first = n - f.n_blocks
+    assert B.q4kv_pool_bytes(spec, n) * (layers - 1) // layers > 2 ** 32
+    big = H.DeviceCache(layers, *shape, False, n, np.where(f.tables >= 0, f.tables + first, -1).astype(np.int32))
+    # the small pool has one layer; it goes to the big one's last through a pool of as many layers
+    mid = torch.zeros(B.q4kv_pool_bytes(spec, f.n_blocks), dtype=torch.uint8, device="cuda")
+    mid[f.dc.pool.numel() * (layers - 1):] = f.dc.pool
+    copies = H.dev(np.array([(i, first + i, 256) for i in range(f.n_blocks)], np.int32))
+    B.q4kv_copy_blocks(spec, mid, f.n_blocks, big.pool, n, layers - 1, 1, copies, f.n_blocks, big.flags)
+    far, far_lse = big.shared_prefix_decode(layers - 1, f.lens, f.offs, f.prefix, q, scale)
+    assert big.read_flags() == 0 and torch.equal(far, out) and torch.equal(far_lse, lse)
+
+
+@pytest.mark.gpu
 def test_the_largest_batch_and_runs_that_repeat():
     """512 agents in uneven groups; the same bits every time, from a workspace that other calls have used, eager and replayed."""
     r = np.random.default_rng(4)
