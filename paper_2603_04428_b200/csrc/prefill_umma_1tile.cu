@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
     {
       // ---- stage this thread's half of the query row: bf16 -> binary16 times a power of two, element order
       //      (0,4,1,5,2,6,3,7) inside every eight ----
-      constexpr int kQWords = kD / 4;                    // packed binary16 words of this thread's half row: 64 or 48
+      constexpr int kQWords = kD / 4;                    // packed binary16 words of this thread's half row: 64, 48 or 32
       const uint16_t* qrow = P.q + ((size_t)(q0 + (valid ? i : 0)) * y.Hq + (size_t)hk * n_rep + h) * kD + (kD / 2) * half;
       uint32_t qa[kQWords];
       float mx = 0.f;
@@ -427,9 +427,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_1tile_kernel(const _
         qa[4 * w + 2] = f32x2_to_h2(x2, x6); qa[4 * w + 3] = f32x2_to_h2(x3, x7);
       }
       // 32-column stores start at multiples of 32 columns, 16-column stores at multiples of 16
-      if (kQWords == 64) {
+      if constexpr (kQWords == 64) {
         tmem_st32(lane_addr + kColQ + 64 * half, qa);
         tmem_st32(lane_addr + kColQ + 64 * half + 32, qa + 32);
+      } else if constexpr (kQWords == 32) {
+        tmem_st32(lane_addr + kColQ + 32 * half, qa);
       } else if (half == 0) {
         tmem_st32(lane_addr + kColQ, qa);
         tmem_st16(lane_addr + kColQ + 32, qa + 32);
@@ -618,6 +620,7 @@ cudaError_t launch_prefill_umma_1tile(const Layout& y, const void* pool, int n_b
   P.q = (const uint16_t*)q; P.scale_log2 = scale * kLog2e; P.out = out; P.out_dtype = out_dtype; P.lse = lse; P.flags = flags;
   P.x = x;
   auto of = [&](auto launch_bf, auto launch_half) { return y.sb_bf16 ? launch_bf(P, max_q_len, st) : launch_half(P, max_q_len, st); };
+  if (x.agent_lens && y.D == 128) return of(launch_shape<2, 2, true, true>, launch_shape<2, 2, false, true>);
   if (x.agent_lens)
     return y.D == 256 ? of(launch_shape<4, 4, true, true>, launch_shape<4, 4, false, true>) : of(launch_shape<3, 2, true, true>, launch_shape<3, 2, false, true>);
   return y.D == 256 ? of(launch_shape<4, 4, true, false>, launch_shape<4, 4, false, false>) : of(launch_shape<3, 2, true, false>, launch_shape<3, 2, false, false>);

@@ -947,10 +947,14 @@ enum class Route { kAlone, kList, kTiles };
 // tiles and stops at 16, 115 us a call instead of 88); 32 of 64 / 1 heads on 32000: 41.8 us instead of 56.4.
 constexpr int kMaxTileSplits = 128;
 struct TilePlan { int splits; double units; };
-int tile_queries(const Layout& y) { return prefill_umma_supported(y) ? 2 * (128 / y.n_rep) : 128 / y.n_rep; }
+bool may_tile(const Layout& y) { return prefill_umma_supported(y) || prefill_umma_1tile_supported(y); }
+// d = 128: two tiles of 128 rows to a CTA, or one where the average group has no more rows (8 KV heads of 4, 8 agents on 32000 tokens: 40.5 us
+// a call, with two tiles 49.4; 8 in each of 3 groups on 8000 34.0 and 42.0)
+bool two_tiles(const Layout& y, int n_agents, int n_groups) { return prefill_umma_supported(y) && (long long)n_agents * y.n_rep > 128ll * n_groups; }
 TilePlan plan_tiles(const Layout& y, int n_agents, int n_groups, int max_kv_len, size_t bytes) {
   const long long sms = sm_count();
-  const long long ctas = (n_groups + (long long)(n_agents - n_groups) / tile_queries(y)) * y.Hkv;     // at most, however groups are cut
+  const int queries = (two_tiles(y, n_agents, n_groups) ? 2 : 1) * (128 / y.n_rep);
+  const long long ctas = (n_groups + (long long)(n_agents - n_groups) / queries) * y.Hkv;     // at most, however groups are cut
   const double blocks = max_kv_len / 64 + 1, merge = 1e-6 * prefill_record_bytes(y, n_agents, 1) / (4. * 1.3);
   TilePlan best = {1, 1e30};
   for (int s = 1; s <= kMaxTileSplits; ++s) {
@@ -966,29 +970,32 @@ TilePlan plan_tiles(const Layout& y, int n_agents, int n_groups, int max_kv_len,
 // of one agent.  alone: a fixed part, m for every agent and every 8 (d = 128) or 4 query heads to a KV head, and the merge by output rows.
 // list: m for every group and every 32 score rows (16 at d = 256; 16 or fewer at the other dimensions cost three quarters).  tiles: the
 // plan's units.  Fitted to 330 measured cases of 2 to 96 agents in 1 or 3 groups on 2000 to 32000 shared tokens with 200 of their own, 1
-// to 64 query heads to a KV head: the choice costs 0.4 % over the best of the three on average, 26 % at most.  Measured alone / list /
+// to 64 query heads to a KV head: the choice costs 0.6 % over the best of the three on average, 26 % at most.  Measured alone / list /
 // tiles, one group unless said otherwise:
-//   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  27.4      32 agents on 32000         206.4 / 99.4 / 52.2
-//   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  27.4      on 32000                    58.0 / 32.1 / 49.5
-//   8 KV heads of 8, d = 128, 16 agents in each of 3 on 8000  107.3 / 100.2 /  71.8      2 agents on 2000: alone in every shape
-//   8 KV heads of 2, d = 256, 16 agents on 32000              220.5 /  76.4 /  64.9      on 2000                     24.8 / 27.3 / 28.6
-//   16 KV heads of 1, d = 192 and 128, 32 agents on 8000      132.6 /  53.6 /  42.2      on 2000                     46.3 / 39.5 / 34.7
+//   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  23.7      32 agents on 32000         206.4 / 99.4 / 43.7
+//   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  23.8      on 32000                    58.0 / 32.1 / 40.2
+//   8 KV heads of 8, d = 128, 16 agents in each of 3 on 8000  107.3 / 100.2 /  71.3      2 agents on 2000: alone in every shape
+//   8 KV heads of 2, d = 256, 16 agents on 32000              220.5 /  76.4 /  64.6      on 2000                     24.8 / 27.3 / 28.0
+//   16 KV heads of 1, d = 192 and 128, 32 agents on 8000      132.6 /  53.6 /  42.3      on 2000                     46.3 / 39.5 / 34.7
 struct RouteCost {
   double alone[3], list[3], tiles[3];      // fixed, a megabyte (tiles: a unit), a thousand output rows
 };
 Route route_of(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool tiles_allowed) {
   if (n_groups >= n_agents) return Route::kAlone;        // nothing is shared
-  constexpr RouteCost k128 = {{7., .185, 3.}, {18., .54, 5.}, {12., 1.14, 4.}}, k192 = {{7., .165, 3.}, {20., .5, 12.}, {12., .96, 7.}},
+  constexpr RouteCost k128 = {{7., .185, 3.}, {18., .54, 5.}, {12., 1.13, 4.}}, k192 = {{7., .165, 3.}, {20., .5, 12.}, {12., .96, 7.}},
                       k256 = {{9., .18, 5.}, {23., .3, 9.}, {17.4, 1.25, 8.3}};
+  constexpr double kOneTile = 0.89;                      // a unit of the one-tile kernel at d = 128
   const RouteCost& k = y.D == 128 ? k128 : y.D == 192 ? k192 : k256;
   const double m = 1e-6 * y.chunk_bytes / kChunkTokens * y.Hkv * max_kv_len, all = 1e-3 * n_agents * y.Hq;
   const double rows = (double)n_agents * y.n_rep / n_groups;             // of an average group and KV head
   const double passes = y.D == 256 ? ceil(rows / 16.) : rows <= 16. ? 0.75 : ceil(rows / 32.);
   const double alone = k.alone[0] + k.alone[1] * m * n_agents * ceil(y.n_rep / (y.D == 128 ? 8. : 4.)) + k.alone[2] * all;
   const double list = k.list[0] + k.list[1] * m * n_groups * passes + k.list[2] * all;
-  const bool may_tile = tiles_allowed && (prefill_umma_supported(y) || prefill_umma_1tile_supported(y));
-  const double tiles =
-      may_tile ? k.tiles[0] + k.tiles[1] * plan_tiles(y, n_agents, n_groups, max_kv_len, (size_t)-1).units + k.tiles[2] * all : 1e30;
+  double tiles = 1e30;
+  if (tiles_allowed && may_tile(y)) {
+    const double unit = y.D == 128 && !two_tiles(y, n_agents, n_groups) ? kOneTile : k.tiles[1];
+    tiles = k.tiles[0] + unit * plan_tiles(y, n_agents, n_groups, max_kv_len, (size_t)-1).units + k.tiles[2] * all;
+  }
   return alone <= list && alone <= tiles ? Route::kAlone : tiles < list ? Route::kTiles : Route::kList;
 }
 
@@ -1065,7 +1072,7 @@ bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int 
 // Whatever way a call takes: one workspace serves shorter contexts and any softmax scale.
 size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len) {
   const size_t list = sections_of(y, n_agents, n_groups, max_kv_len, Route::kList).end;
-  if (!prefill_umma_supported(y) && !prefill_umma_1tile_supported(y)) return list;
+  if (!may_tile(y)) return list;
   const size_t tiles = sections_of(y, n_agents, n_groups, max_kv_len, Route::kTiles).end;
   return tiles > list ? tiles : list;
 }
@@ -1096,7 +1103,7 @@ cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks
     P.splits = x.n_splits = plan_tiles(y, b.n_agents, n_groups, max_kv_len, workspace_bytes - kWorkspaceHeaderBytes - s.rec_o).splits;
     x.records = P.rec_o; x.agent_lens = kv_lens; x.n_agents = b.n_agents; x.max_kv_len = max_kv_len;
     const q4kv_batch groups = {n_groups, b.max_blocks, b.block_tables};
-    const auto launch = prefill_umma_supported(y) ? launch_prefill_umma : launch_prefill_umma_1tile;
+    const auto launch = two_tiles(y, b.n_agents, n_groups) ? launch_prefill_umma : launch_prefill_umma_1tile;
     e = launch(y, pool, n_blocks, layer, groups, prefix_lens, group_offs, b.n_agents, 0, q, scale, nullptr, Q4KV_OUT_F32, nullptr, flags, st, x);
   } else {
     e = y.D == 128 ? launch_list<2, 2>(P, st) : y.D == 256 ? launch_list<4, 4>(P, st) : launch_list<3, 2>(P, st);

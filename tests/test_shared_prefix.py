@@ -151,7 +151,7 @@ def test_many_query_heads_to_a_kv_head(shape, more):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("groups", [[(700, [1, 90, 300]), (40, [5])], [(700, [i % 5 for i in range(8)])], [(700, [i % 5 for i in range(70)])]])
+@pytest.mark.parametrize("groups", [[(700, [1, 90, 300]), (40, [5])], [(700, [i % 5 for i in range(8)])], [(700, [i % 5 for i in range(24)])], [(700, [i % 5 for i in range(70)])]])
 @pytest.mark.parametrize("shape", [(8, 2, 128, 128), (2, 2, 192, 128), (4, 2, 256, 256)])
 def test_bfloat16_scales_and_bfloat16_output(shape, groups):
     f = Forked(shape, groups, seed=33, sb_dtype=1, layers=2, wide=WIDE)
