@@ -34,6 +34,7 @@
 // as they are a block takes 2100).  With one barrier for all eight softmax warps, maxima exchanged in every block and 96
 // registers for every warp (the d = 256 form spilled) it took 3400.  8 agents x (4096 + 512) tokens, 16 query heads, d = 256:
 // 508 -> 382 us (575 -> 765 TFLOP/s) in a run of seconds, 363 us in one of a few launches; 192 / 128: 350 -> 282 (648), 281.
+// The form for groups of agents that share a prefix (kGroups) also exists at d = 128, for groups of up to 128 rows.
 // With the output stored a line at a time (store_rows): 371 (788) and 354; 192 / 128: 275 (665) and 278.
 #include "prefill_common.cuh"
 

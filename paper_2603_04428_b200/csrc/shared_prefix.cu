@@ -958,8 +958,8 @@ TilePlan plan_tiles(const Layout& y, int n_agents, int n_groups, int max_kv_len,
   const double blocks = max_kv_len / 64 + 1, merge = 1e-6 * prefill_record_bytes(y, n_agents, 1) / (4. * 1.3);
   TilePlan best = {1, 1e30};
   for (int s = 1; s <= kMaxTileSplits; ++s) {
-    // the kernel numbers blocks times parts in 32 bits
-    if (s > 1 && (s * 4 > blocks || (s + 1) * blocks > 2147483647. || prefill_record_bytes(y, n_agents, s) > bytes)) break;
+    // the kernel numbers blocks times parts in 32 bits, a grid's second dimension in 16
+    if (s > 1 && (s * 4 > blocks || (long long)y.Hkv * s > 65535 || (s + 1) * blocks > 2147483647. || prefill_record_bytes(y, n_agents, s) > bytes)) break;
     const double t = (double)((ctas * s + sms - 1) / sms) * (blocks / s + 4.) + s * merge;
     if (t < 0.97 * best.units) best = {s, t};
   }
