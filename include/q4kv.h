@@ -251,7 +251,7 @@ int q4kv_decode_attention_layers(const q4kv_spec* spec, void* pool, int32_t n_bl
  *   max_kv_len   as for q4kv_decode_attention; which way a call takes is estimated from it, n_agents and n_groups, so a bound near
  *                the lengths serves best
  *   workspace    at least q4kv_workspace_bytes_shared_prefix bytes, its header zeroed once as for q4kv_decode_attention, which may
- *                share it
+ *                share it.  One made for the most agents, groups and the longest context serves smaller calls
  * Like the other lengths, group_offs and prefix_lens are read before the preceding kernels of the stream have completed.
  * A bad block gives zeros for every agent that reads it: one of the prefix for all the agents that read it through that row, one
  * among an agent's own blocks for that agent.  Sliding windows have no argument here: their layers attend few keys each

@@ -278,7 +278,7 @@ int q4kv_shared_prefix_decode_attention(const q4kv_spec* spec, const void* pool,
   if (max_kv_len == 0 || max_kv_len > cap) max_kv_len = cap;
   const Layout y = make_layout(*spec, n_blocks);
   if (!shared_prefix_supported(y, batch->n_agents, batch->max_blocks, max_kv_len) || spec->exact_products != 0) return Q4KV_EUNSUPPORTED;
-  if (workspace_bytes < kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, batch->n_agents, n_groups, max_kv_len)) return Q4KV_EWORKSPACE;
+  if (workspace_bytes < kWorkspaceHeaderBytes + shared_prefix_workspace_bytes(y, batch->n_agents, n_groups, max_kv_len, true)) return Q4KV_EWORKSPACE;
   const cudaError_t e = launch_shared_prefix(y, pool, n_blocks, layer, *batch, kv_lens, max_kv_len, group_offs, prefix_lens, n_groups, q,
                                              softmax_scale, tiles_allowed(spec, softmax_scale), out, out_dtype, lse, workspace,
                                              workspace_bytes, status_flags, (cudaStream_t)stream);

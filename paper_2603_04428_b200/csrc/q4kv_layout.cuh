@@ -212,7 +212,7 @@ cudaError_t launch_merge_prefill(const Layout& y, int total_q, int n_splits, con
 
 // Decode of agents that share prefixes (d_qk = d_v in {128, 256}, d_qk 192 / d_v 128)
 bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int max_kv_len);
-size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len);
+size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool least = false);
 cudaError_t launch_shared_prefix(const Layout& y, const void* pool, int n_blocks, int layer, const q4kv_batch& b, const int32_t* kv_lens,
                                  int max_kv_len, const int32_t* group_offs, const int32_t* prefix_lens, int n_groups, const void* q,
                                  float scale, bool tiles_allowed, void* out, int out_dtype, float* lse, void* workspace,

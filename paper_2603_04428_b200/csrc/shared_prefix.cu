@@ -1069,12 +1069,14 @@ bool shared_prefix_supported(const Layout& y, int n_agents, int max_blocks, int 
          (2ll * n_agents * y.Hq / max_rows_of(y) + n_agents * y.Hkv) * (max_kv_len / 128 + 2 + kSegmentCost) < (1ll << 30);
 }
 
-// Whatever way a call takes: one workspace serves shorter contexts and any softmax scale.
-size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len) {
+// Whatever way a call takes, with as many parts of the tiles' keys as are planned.  least: with one part, which is what a call has to
+// have; it grows with the agents and groups and does not depend on the lengths, so that one workspace serves smaller calls too.
+size_t shared_prefix_workspace_bytes(const Layout& y, int n_agents, int n_groups, int max_kv_len, bool least) {
   const size_t list = sections_of(y, n_agents, n_groups, max_kv_len, Route::kList).end;
   if (!may_tile(y)) return list;
-  const size_t tiles = sections_of(y, n_agents, n_groups, max_kv_len, Route::kTiles).end;
-  return tiles > list ? tiles : list;
+  const Sections tiles = sections_of(y, n_agents, n_groups, max_kv_len, Route::kTiles);
+  const size_t end = least ? tiles.rec_o + prefill_record_bytes(y, n_agents, 1) : tiles.end;
+  return end > list ? end : list;
 }
 
 // workspace: with its header (the decode launch's arrival counters)

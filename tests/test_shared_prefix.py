@@ -318,6 +318,29 @@ def test_blocks_beyond_four_gigabytes(shape, wide, more):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(4, 1, 128, 128), (2, 1, 256, 256)])
+def test_a_workspace_for_the_largest_call_serves_smaller_ones(shape):
+    """Fewer agents can be cut into more parts, which need more room than the largest batch's plan: parts follow the room."""
+    from paper_2603_04428_b200 import harness as H
+    f = Forked(shape, [(3000, [i % 4 for i in range(65)])], seed=42, wide=WIDE)
+    q, scale, dc, most = f.q(), 1.0 / math.sqrt(shape[2]), f.dc, WIDE * 256
+    want, want_lse = f.want(q, scale)
+    room = B.q4kv_workspace_bytes_shared_prefix(dc.spec, 65, most, 1)
+    assert B.q4kv_workspace_bytes_shared_prefix(dc.spec, 64, most, 1) > room          # or nothing is tested here
+    ws = torch.zeros(room, dtype=torch.uint8, device="cuda")
+    qd, lens, pre = H.bf16_dev(q), H.dev(np.asarray(f.lens, np.int32)), H.dev(np.asarray(f.prefix, np.int32))
+    for a, longest in ((65, most), (64, most), (33, most), (64, 100000), (64, 20000), (64, 4096), (5, 4096), (1, 4096)):
+        out = torch.full((65, shape[0], shape[3]), 9.0, device="cuda")
+        lse = torch.full((65, shape[0]), 9.0, device="cuda")
+        offs = H.dev(np.array([0, a], np.int32))
+        B.q4kv_shared_prefix_decode_attention(dc.spec, dc.pool, f.n_blocks, 0, B.Batch(a, WIDE, dc.bt.block_tables), lens, longest, offs,
+                                              pre, 1, qd, scale, out, B.OUT_F32, lse, ws, dc.flags)
+        close(out[:a], lse[:a], want[:a], want_lse[:a])
+        assert torch.all(out[a:] == 9.0) and torch.all(lse[a:] == 9.0)                # rows behind the last agent
+    assert dc.read_flags() == 0 and int(ws[:B.WORKSPACE_HEADER_BYTES].max()) == 0
+
+
+@pytest.mark.gpu
 def test_the_largest_batch_and_runs_that_repeat():
     """512 agents in uneven groups; the same bits every time, from a workspace that other calls have used, eager and replayed."""
     r = np.random.default_rng(4)
