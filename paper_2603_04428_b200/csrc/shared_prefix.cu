@@ -5,8 +5,9 @@
 //   m_i = a reference for its scores, l_i = sum 2^(s - m_i), o_i = sum 2^(s - m_i) v, and
 //   out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i with M = max m_i.
 //
-// Three launches: the prefixes (here), the agents' own tokens (decode_mma, its range beginning behind the prefix), the sum of the parts
-// (here).
+// Three launches: the prefixes (here, or on the prefill kernels where many rows share one), the agents' own tokens (decode_mma, its
+// range beginning behind the prefix), the sum of the parts (here).  Where that takes longer than every agent reading its own keys, one
+// launch of decode_mma does (route_of).
 //
 // The prefixes' work is a list of segments (group, tile of score rows, KV head) with up to kRows rows each, cut into equal contiguous
 // ranges of 128-key steps, one per CTA and one CTA per SM; every CTA leaves a record per segment that it touched.  One step is two
