@@ -299,9 +299,10 @@ def q4kv_shared_prefix_decode_attention(spec, pool, n_blocks, layer, bt: Batch, 
 def q4kv_norm_rope(spec, how: NormRotation, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags=None):
     """Norm and rotation of the new query and key rows.  q, k: bfloat16 [total_new][heads][d_qk] whose first stride is free (a
     view of a fused projection); q_out, k_out contiguous, or the input itself."""
-    assert how.device is None or how.device == _device(), "a tensor lies on another device than the current one"
-    _check(_native().norm_rope(spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, _stream(),
-                               _device()), "q4kv_norm_rope")
+    device = _device()
+    assert how.device is None or how.device == device, "a tensor lies on another device than the current one"
+    _check(_native().norm_rope(spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, _stream(), device),
+           "q4kv_norm_rope")
 
 
 def q4kv_copy_blocks(spec, src_pool, src_blocks, dst_pool, dst_blocks, layer_begin, layer_count, copies, n_copies,

@@ -29,13 +29,21 @@ static int (*f_shared_prefix)(const q4kv_spec*, const void*, int32_t, int32_t, c
 static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes, *s_get_device, *s_stride, *s_element_size;
 
 /* A device pointer: None, an integer, or a contiguous CUDA tensor. */
-static int get_ptr(PyObject* o, void** out) {
+static int on_device(PyObject* o, long dev);
+/* dev: the device that a tensor has to lie on (which also says that it is a CUDA tensor), or kAnyDevice */
+enum { kAnyDevice = -1 };
+static int get_ptr_at(PyObject* o, long dev, void** out) {
   if (o == Py_None) { *out = NULL; return 1; }
   if (PyLong_Check(o)) { *out = PyLong_AsVoidPtr(o); return !(*out == NULL && PyErr_Occurred()); }
-  PyObject* r = PyObject_GetAttr(o, s_is_cuda);
-  if (!r) return 0;
-  int ok = PyObject_IsTrue(r);
-  Py_DECREF(r);
+  PyObject* r;
+  int ok = 1;
+  if (dev == kAnyDevice) {
+    if (!(r = PyObject_GetAttr(o, s_is_cuda))) return 0;
+    ok = PyObject_IsTrue(r);
+    Py_DECREF(r);
+  } else if (!on_device(o, dev)) {
+    return 0;
+  }
   if (ok > 0) {
     if (!(r = PyObject_CallMethodNoArgs(o, s_is_contiguous))) return 0;
     ok = PyObject_IsTrue(r);
@@ -48,6 +56,7 @@ static int get_ptr(PyObject* o, void** out) {
   Py_DECREF(r);
   return !(*out == NULL && PyErr_Occurred());
 }
+static int get_ptr(PyObject* o, void** out) { return get_ptr_at(o, kAnyDevice, out); }
 static int get_i32(PyObject* o, int32_t* out) {
   const unsigned long v = PyLong_AsUnsignedLongMask(o);
   *out = (int32_t)(uint32_t)v;
@@ -164,20 +173,18 @@ static int on_device(PyObject* o, long dev) {
   if (at != dev) { PyErr_SetString(PyExc_AssertionError, "a tensor lies on another device than the current one"); return 0; }
   return 1;
 }
-static int get_ptr_on(PyObject* o, long dev, void** out) { return get_ptr(o, out) && on_device(o, dev); }
+static int get_ptr_on(PyObject* o, int32_t dev, void** out) {
+  if (dev < 0) { PyErr_SetString(PyExc_AssertionError, "no such device"); return 0; }
+  return get_ptr_at(o, dev, out);
+}
 /* Rows [tokens][heads][d] of 16-bit elements whose first stride is free: pointer and stride. */
 static int get_rows(PyObject* o, long dev, void** out, int64_t heads, int64_t d, int64_t rows, int64_t* stride) {
   int64_t st[3];
   PyObject* r;
   *stride = heads * d;
   if (o == Py_None) { *out = NULL; return 1; }
-  if (!(r = PyObject_GetAttr(o, s_is_cuda))) return 0;
-  int ok = PyObject_IsTrue(r);
-  Py_DECREF(r);
-  if (ok < 0) return 0;
-  if (!ok) { PyErr_SetString(PyExc_AssertionError, "rows come from CUDA tensors"); return 0; }
   if (!on_device(o, dev) || !(r = PyObject_CallMethodNoArgs(o, s_stride))) return 0;
-  ok = PyArg_ParseTuple(r, "LLL", &st[0], &st[1], &st[2]);
+  int ok = PyArg_ParseTuple(r, "LLL", &st[0], &st[1], &st[2]);
   Py_DECREF(r);
   if (!ok) return 0;
   if (!(r = PyObject_CallMethodNoArgs(o, s_element_size))) return 0;
