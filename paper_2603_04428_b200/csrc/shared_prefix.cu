@@ -1009,9 +1009,7 @@ Sections sections_of(const Layout& y, int n_agents, int n_groups, int max_kv_len
   s.own_lse = align256(decode_mma_workspace_bytes(y, n_agents));
   s.own_o = s.own_lse + align256(q_rows * sizeof(float));
   s.rec_ml = s.own_o + align256(q_rows * y.Dv * sizeof(float));
-  if (route == Route::kAlone) {
-    s.rec_ml = s.rec_o = s.end = s.own_lse;
-  } else if (route == Route::kTiles) {
+  if (route == Route::kTiles) {
     s.rec_o = s.rec_ml;
     s.end = s.rec_o + align256(prefill_record_bytes(y, n_agents, plan_tiles(y, n_agents, n_groups, max_kv_len, (size_t)-1).splits));
   } else {
