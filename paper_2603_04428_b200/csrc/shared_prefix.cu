@@ -284,11 +284,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
       // =============================== segments and raw steps =====================================
       // (lengths, offsets and block tables are inputs that no kernel writes)
       int total = 0;
+      bool ascending = true;                             // else groups can overlap: more tiles than there are records, or positions
 #pragma unroll 1
-      for (int base = 0; base < P.n_groups; base += 32) {
-        const Group q = group_of<kRows>(P, base + lane);
+      for (int base = 0; base < P.n_groups && ascending; base += 32) {
+        bool fine = true;
+        const Group q = group_of<kRows>(P, base + lane, &fine);
+        ascending = __all_sync(0xffffffffu, fine);
         total += __reduce_add_sync(0xffffffffu, q.tiles * y.Hkv * q.cost);
       }
+      if (!ascending) total = 0;                         // no work; the merge reports it
       const Cut cut(total, gridDim.x);
       const bool any = (int)blockIdx.x < cut.n && total > 0;
       const int u0 = any ? cut.begin(blockIdx.x) : 0, u1 = any ? cut.begin(blockIdx.x + 1) : 0;

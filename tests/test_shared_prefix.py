@@ -260,6 +260,46 @@ def test_lengths_that_cannot_be_raise_the_flag_and_give_zeros(wide, more):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("sharp", [1.0, 2.5])
+@pytest.mark.parametrize("n_groups", [8, 20, 31])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
+def test_groups_that_overlap_stay_inside_the_workspace(shape, n_groups, sharp):
+    """Offsets 0, A, 0, A, ...: every second group is in order by itself and names all agents.  Together they have several times the
+    score rows that the workspace was sized for, so nothing may be computed for them.  The workspace is as small as the call accepts."""
+    from paper_2603_04428_b200 import harness as H
+    A, longest = 64, WIDE * 256
+    f = Forked(shape, [(1500, [i % 3 for i in range(A)])], seed=43, wide=WIDE)
+    dc, scale = f.dc, sharp / math.sqrt(shape[2])
+    offs = H.dev(np.array([A * (i % 2) for i in range(n_groups + 1)], np.int32))
+    lens, pre, q = H.dev(np.asarray(f.lens, np.int32)), H.dev(np.full(n_groups, 1500, np.int32)), H.bf16_dev(f.q())
+    out, lse = torch.empty((A, shape[0], shape[3]), device="cuda"), torch.empty((A, shape[0]), device="cuda")
+    most = B.q4kv_workspace_bytes_shared_prefix(dc.spec, A, longest, n_groups)
+    room = torch.zeros(most + (64 << 20), dtype=torch.uint8, device="cuda")
+
+    def call(size):
+        out.fill_(9.0)
+        lse.fill_(9.0)
+        dc.flags.zero_()
+        room[B.WORKSPACE_HEADER_BYTES:] = 0xA5
+        B.q4kv_shared_prefix_decode_attention(dc.spec, dc.pool, f.n_blocks, 0, dc.bt, lens, longest, offs, pre, n_groups, q, scale, out,
+                                              B.OUT_F32, lse, room[:size], dc.flags)
+        assert torch.all(room[size:] == 0xA5) and int(room[:B.WORKSPACE_HEADER_BYTES].max()) == 0
+        assert dc.read_flags() == B.FLAG_BAD_LENGTH and torch.all(out == 0) and torch.all(torch.isneginf(lse))
+
+    low, high = 0, most                                  # the least size that is accepted
+    while high - low > 1:
+        size = (low + high) // 2
+        try:
+            call(size)
+            high = size
+        except B.Q4KVError as e:
+            assert e.code == B.EWORKSPACE
+            low = size
+    call(high)
+    call(most)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("wide, more", [(1, 0), (WIDE, 4), (WIDE, 80)])
 def test_bad_blocks_spoil_the_agents_that_read_them(wide, more):
     f = Forked((8, 2, 128, 128), [(600, [20, 300, 9] + [1] * more), (40, [100, 3])], seed=37, wide=wide)
