@@ -705,6 +705,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             if (!set_any(set, most > kGrow) || grown) break;
             fence_after_sync();
           } else if (mine == 0) {
+            // a set without rows: all of its warps have seen this step's scores before one arrives for the set, or a warp that is behind
+            // could find that barrier two phases on and wait for good
+            set_sync(set);
             break;
           }
           // the references of the rows that outgrow theirs (of all, in the first step) move above the maximum of this step's scores; the

@@ -202,6 +202,19 @@ def test_references_that_have_to_move(shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape, agents", [((4, 2, 128, 128), 4), ((4, 4, 192, 128), 8), ((4, 2, 256, 256), 3)])
+def test_groups_of_at_most_eight_rows(shape, agents):
+    """Half of the softmax warps have no rows then, and may be behind the others in any step: many steps, call after call."""
+    f = Forked(shape, [(9000, [i % 3 for i in range(agents)])], seed=44, wide=WIDE)
+    q, scale = f.q(), 2.5 / math.sqrt(shape[2])
+    out, lse = f.run(q, scale)
+    close(out, lse, *f.want(q, scale))
+    for _ in range(300):
+        again, again_lse = f.run(q, scale)
+    assert torch.equal(again, out) and torch.equal(again_lse, lse) and f.dc.read_flags() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("more", [0, 4, 60])
 def test_one_agents_bad_query_leaves_the_others_alone(more):
     f = Forked((8, 2, 128, 128), [(600, [20, 30, 1, 0] + [2] * more)], seed=35, wide=WIDE)
