@@ -95,7 +95,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mla_kernel(const __grid_c
   const int q0 = P.q_offs[a], q_len = P.q_offs[a + 1] - q0;
   const int kv_len = P.kv_lens[a];
   const int i_min = qt * tile_q;
-  if (i_min >= q_len) return;                            // uniform: nothing allocated, no barrier passed
+  if (i_min >= q_len) {                                  // uniform: nothing allocated, no barrier passed
+    hold_stream_order();
+    return;
+  }
   const bool bad_len = kv_len < 0 || kv_len > P.max_blocks * kBlockTokens || q_len > kv_len;
   const int i_max = min(q_len, i_min + tile_q) - 1;
   const int prefix = kv_len - q_len;                     // query i sits at position prefix + i

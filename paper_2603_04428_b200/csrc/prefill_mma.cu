@@ -127,7 +127,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
   const int hs = n_rep > 2 ? 4 : n_rep;
   const int tile_q = (kWarps / hs) * 16 * R;             // queries per CTA
   const int i_min = qt * tile_q;
-  if (i_min >= q_len) return;                            // uniform: no thread has passed a barrier yet
+  if (i_min >= q_len) {                                  // uniform: no thread has passed a barrier yet
+    hold_stream_order();
+    return;
+  }
   const bool bad_len = kv_len < 0 || kv_len > P.max_blocks * kBlockTokens || q_len > kv_len;
   if (bad_len && threadIdx.x == 0) raise_flag(P.flags, Q4KV_FLAG_BAD_LENGTH);
   const int i_max = min(q_len, i_min + tile_q) - 1;

@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_umma_kernel(const __grid_
   const int i_min = qt * 2 * tile_q;
   if (P.x.tickets && qt == 0 && blockIdx.y == 0 && a == 0) clear_tickets(P.x);
   if (i_min >= q_len || (P.x.tickets && q_len == 1)) {         // uniform: nothing allocated, no barrier passed
-    if (kGroups) asm volatile("griddepcontrol.wait;" ::: "memory");    // or a grid without rows could complete before the one it follows
+    hold_stream_order();
     return;
   }
   const bool bad_len = kv_len < 0 || kv_len > (kGroups ? P.x.max_kv_len : P.max_blocks * kBlockTokens) || (!kGroups && q_len > kv_len);

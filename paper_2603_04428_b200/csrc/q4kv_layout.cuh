@@ -106,6 +106,12 @@ __device__ inline uint8_t* head_block(void* pool, const Layout& y, int layer, in
          (uint64_t)kv_head * y.head_block_bytes;
 }
 
+// For CTAs that leave because they have nothing to do.  A kernel waits for the grid before it only; if none of that grid's CTAs waited
+// for the one before, that one's writes may be missing.  One CTA that waits is enough: its grid is not complete before it.
+__device__ inline void hold_stream_order() {
+  if ((blockIdx.x | blockIdx.y | blockIdx.z) == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 __device__ inline void raise_flag(int32_t* status_flags, int bit) {
   if (status_flags) atomicOr(status_flags, bit);
 }

@@ -315,3 +315,34 @@ def test_a_call_without_work_does_not_let_its_successor_overtake_its_predecessor
         B.q4kv_copy_blocks(spec, b, n, c, n, 0, 2, last, 40)
         got, want = (t.view(2, n, 8, 8, -1)[:, n - 40:] for t in (c, a))
         assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("agents", [1, 3, 40])
+@pytest.mark.parametrize("shape, sharp", [((8, 2, 128, 128, False), 1.0), ((8, 2, 256, 256, False), 1.0), ((4, 4, 192, 128, False), 1.0),
+                                          ((16, 1, 576, 512, True), 1.0), ((8, 2, 128, 128, False), 2.5), ((8, 2, 256, 256, False), 2.5),
+                                          ((4, 2, 64, 64, False), 1.0)])
+def test_a_prefill_without_queries_does_not_let_its_successor_overtake_its_predecessor(shape, sharp, agents):
+    """As above, for a prefill call in which no agent has a query (a step of a captured schedule with nothing to do)."""
+    n = 1500
+    spec, a, _ = _pool((2, 32, 8, 128, 128, False), n, 5)
+    b, c = torch.zeros_like(a), torch.zeros_like(a)
+    every = torch.tensor([(i, i, 256) for i in range(n)], dtype=torch.int32, device="cuda")
+    last = torch.tensor([(i, i, 256) for i in range(n - 40, n)], dtype=torch.int32, device="cuda")
+    other = B.Spec.make(1, *shape)
+    rows, width = 64, 64
+    pool = torch.zeros(B.q4kv_pool_bytes(other, 2), dtype=torch.uint8, device="cuda")
+    q = torch.zeros((rows, shape[0], shape[2]), dtype=torch.bfloat16, device="cuda")
+    out = torch.full((rows, shape[0], shape[3]), 9.0, dtype=torch.bfloat16, device="cuda")
+    tables, zeros = torch.zeros((agents, width), dtype=torch.int32, device="cuda"), torch.zeros(256, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(B.q4kv_workspace_bytes(other, agents, width * 256, rows), dtype=torch.uint8, device="cuda")
+    bt = B.Batch(agents, width, tables.data_ptr())
+    for _ in range(10):
+        b.zero_()
+        c.zero_()
+        B.q4kv_copy_blocks(spec, a, n, b, n, 0, 2, every, n)
+        B.q4kv_prefill_attention(other, pool, 2, 0, bt, zeros, zeros, rows, rows, width * 256, 0, q, sharp / shape[2] ** 0.5, out,
+                                 B.OUT_BF16, None, ws)
+        B.q4kv_copy_blocks(spec, b, n, c, n, 0, 2, last, 40)
+        got, want = (t.view(2, n, 8, 8, -1)[:, n - 40:] for t in (c, a))
+        assert torch.equal(got, want)
