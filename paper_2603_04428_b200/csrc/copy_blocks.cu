@@ -20,7 +20,8 @@ copy_blocks_kernel(uint32_t chunk_bytes, int heads, const uint8_t* src, int src_
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int i = blockIdx.x / heads, hk = blockIdx.x % heads, layer = layer0 + blockIdx.y;
-  const int from = copies[3 * i], to = copies[3 * i + 1], n = copies[3 * i + 2];
+  const int32_t* const mine = copies + 3 * (size_t)i;    // a long list passes 32 bits
+  const int from = mine[0], to = mine[1], n = mine[2];
   const bool bad_block = from < 0 || from >= src_blocks || to < 0 || to >= dst_blocks, bad_length = n < 0 || n > kBlockTokens;
   if (bad_block || bad_length) {
     if (threadIdx.x == 0) raise_flag(flags, (bad_block ? Q4KV_FLAG_BAD_BLOCK : 0) | (bad_length ? Q4KV_FLAG_BAD_LENGTH : 0));

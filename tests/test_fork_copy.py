@@ -236,6 +236,21 @@ def test_a_captured_copy_replays_with_the_list_of_the_moment():
 
 
 @pytest.mark.gpu
+def test_a_list_of_copies_beyond_two_gigaentries():
+    """The list's last copies lie past entry 2^31; those before them copy nothing."""
+    n = 2 ** 31 // 3 + 20
+    spec = B.Spec.make(1, 1, 1, 128, 128)
+    pool = torch.randint(0, 256, (B.q4kv_pool_bytes(spec, 40),), dtype=torch.uint8, device="cuda")
+    t = torch.zeros((n, 3), dtype=torch.int32, device="cuda")
+    t[-20:] = torch.tensor([(i, 20 + i, 256) for i in range(20)], dtype=torch.int32)
+    flags = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want = pool.clone().view(40, -1)
+    want[20:] = want[:20]
+    B.q4kv_copy_blocks(spec, pool, 40, pool, 40, 0, 1, t, n, flags)
+    assert torch.equal(pool.view(40, -1), want) and int(flags) == 0
+
+
+@pytest.mark.gpu
 def test_forked_agents_hold_what_they_would_have_built_alone():
     """A parent of 600 tokens, a fork at 550, more tokens for both, then compaction: the packed bytes of both equal those of
     agents that appended the same rows by themselves."""
