@@ -257,8 +257,10 @@ int q4kv_decode_attention_layers(const q4kv_spec* spec, void* pool, int32_t n_bl
  * among an agent's own blocks for that agent.  Sliding windows have no argument here: their layers attend few keys each
  * (q4kv_decode_attention).
  * Accuracy: agents by themselves, and agents' own tokens, as q4kv_decode_attention.  Prefixes of groups: the scores are exact
- * products with binary32 sums and each probability times a value's scale is rounded once to binary16; or, where
- * softmax_scale <= 2/sqrt(d_qk) and many query rows share a prefix, the kernels that expand the cache into binary16 tiles.
+ * products with binary32 sums and each probability times a value's scale is rounded once to binary16, which adds at most 2^-11 of a
+ * group's span 15 * scale (2^-10 * M, "Accuracy" above); or, where softmax_scale <= 2/sqrt(d_qk) and many query rows share a
+ * prefix, the kernels that expand the cache into binary16 tiles, with their bound there.  exact_products == 1 has neither: such a
+ * spec makes the q4kv_decode_attention call.
  * Covered: d_qk = d_v in {128, 256} and d_qk 192 / d_v 128, V not aliasing K, exact_products == 0, n_agents * n_kv_heads
  * times the sets of 8 (d_qk = 128) or 4 query heads of a KV head at most 16384, and contexts whose work lists fit 32-bit numbers.
  * Anything else returns Q4KV_EUNSUPPORTED and the caller makes the q4kv_decode_attention call. */

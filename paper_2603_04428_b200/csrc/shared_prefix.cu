@@ -21,6 +21,9 @@
 // divided out of the other operand): five instructions per eight codes, where the expansion to c s + b takes thirteen.  Scores are
 // exact products with binary32 sums; the probabilities times a scale are rounded once to binary16.  (Expanded keys and values, up to
 // 64 rows a segment: 1400 instructions a scheduler and step at N = 16, 2200 clocks, whatever the rows.)
+// Where a key's p s falls below binary16's range its codes are lost while its bias stays, and it counts as its group's minimum: a sink ten
+// nats above the rest and values of 0.01 left a tenth of the output wrong.  So all references of a segment lie lower by as many binary
+// orders as its value scales allow (lift_of): p s has its full 11 bits down to 2^-24 of the largest, 2^-20 for odd tokens.
 // A lane of tensor memory is a key: a softmax thread has one key, its scales and biases in registers, and half of the rows; the mask is
 // a matter of whole lanes.  The sums of p and p b_g stay in the threads' registers until the segment ends.  What a step costs an SM
 // at d = 128: HBM 790 clocks (18.4 KB), tensor pipe 512.
@@ -28,8 +31,8 @@
 //     (bf16 times a power of two per row into binary16, exact).
 //   * Two sets of four warps unpack keys, two values, a set every second step.
 //   * Two sets of four softmax warps share the rows.  The reference m of a row is kMargin above the maximum over the segment's first
-//     step; it moves when a probability would exceed 2^kGrow, which is found by all keys of a set together at the barrier that also
-//     ends the set's stores of P.
+//     step, less the segment's lift; it moves when a probability would exceed 2^kGrow times the lift, or a value scale what the lift
+//     allows, which is found by all keys of a set together at the barrier that also ends the set's stores of P.
 // All waits are bounded; one that runs out raises Q4KV_FLAG_INTERNAL, lets the copies and the tensor pipe drain and gives the
 // tensor memory back.
 #include <cmath>
@@ -47,8 +50,9 @@ constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 16, kLoadWarp = 24, 
 constexpr int kThreads = 28 * 32;
 constexpr int kRegsSoftmax = 112, kRegsOther = 56;       // of the 72 each thread is launched with
 static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + (kThreads - kSoftmaxWarps * 32) * kRegsOther <= kThreads * 72, "");
-constexpr float kGrow = 2.5f;                            // p <= 2^2.5: p s stays below 65504 for every scale the quantizer can write (8734)
+constexpr float kGrow = 2.5f;                            // p <= 2^(2.5 + lift), s <= 2^(13 - lift): p s stays below 65504
 constexpr float kMargin = 1.f;
+constexpr int kSmallest = -40;                           // smaller scales count as 2^-40, so that p stays far from binary32's limits
 constexpr int kInfo = 8;                                 // segments that the loader may be ahead of the softmax
 constexpr int kSegmentCost = 1;                          // of a segment beside its steps, in steps
 
@@ -182,6 +186,7 @@ struct Smem {
   alignas(16) float kappa[2][Sh::kRows], q_sum[2][G][Sh::kRows];
   // of the two softmax sets: minus the reference of each row, what to scale by when it moves, partial maxima, sums of p and p b_g
   alignas(16) float neg_ref[2][Sh::kRows / 2], factor[2][Sh::kRows / 2], red_max[2][4][Sh::kRows / 2], red_sum[2][4][Gv + 1][Sh::kRows / 2];
+  float red_scale[2][4];                                       // the largest value scale of a warp's keys
   alignas(8) uint64_t raw_full[Sh::kRaw], raw_free[Sh::kRaw];
   uint64_t k_full[2], s_full[2], p_full[2], o_done[2], q_full[2], q_free[2], info_full[kInfo], info_free[kInfo], drain;
   Segment info[kInfo];
@@ -241,6 +246,13 @@ __device__ inline float sum_of8(uint4 v) {
 __device__ inline uint4 codes8(uint32_t w, const CodeMasks& m) {
   const uint32_t wh = w >> 8;
   return make_uint4(w & m.lo, w & m.hi, wh & m.lo, wh & m.hi);
+}
+// The binary orders that p may lie above 1, and the largest value scale that allows it, by a segment's largest so far: two to four times
+// that one, so that it seldom has to move.  Powers of two: nothing is rounded by it.
+struct Lift { float orders, limit; };
+__device__ inline Lift lift_of(float scale) {
+  const int e = max((int)(__float_as_uint(scale) >> 23) - 127, kSmallest) + 2;     // scale < 2^(e - 1)
+  return {(float)(13 - e), e < 128 ? __uint_as_float((uint32_t)(127 + e) << 23) : INFINITY};
 }
 template <bool kBf>
 __device__ inline float2 scale_bias(uint32_t u) {
@@ -626,6 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         for (int v = 0; v < Gv; ++v) pb[v][c] = 0ull;
       }
       bool started = false;
+      Lift lift = {0.f, 0.f};
 #pragma unroll 1
       for (int j = 0; j < s.steps; ++j, ++g) {
         const int b = g & 1, r = g % kRaw;
@@ -635,6 +648,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
         wait_for(&sm.raw_full[r], g / kRaw, abort_flag);
         // the key's scales and biases
         uint64_t ks[G], kb[G], vs[Gv], vb[Gv];
+        float largest = 0.f;                             // of its value scales
         {
           const uint8_t* chunk = sm.raw[r] + quad * Sh::kChunkBytes;
 #pragma unroll
@@ -647,6 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
           for (int i = 0; i < Gv; ++i) {
             float2 e = scale_bias<kBf>(*reinterpret_cast<const uint32_t*>(chunk + Sh::kOffVsb + at_sb * Gv + 4 * i));
             if (edge && !valid) e = make_float2(0.f, 0.f);
+            largest = fmaxf(largest, fabsf(e.x));
             vs[i] = pair64(e.x * place, e.x * place);
             vb[i] = pair64(e.y, e.y);
           }
@@ -702,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             }
             fence_async_smem();
             fence_before_sync();
-            if (!set_any(set, most > kGrow) || grown) break;
+            if (!set_any(set, most > kGrow + lift.orders || largest > lift.limit) || grown) break;
             fence_after_sync();
           } else if (mine == 0) {
             // a set without rows: all of its warps have seen this step's scores before one arrives for the set, or a warp that is behind
@@ -711,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
             break;
           }
           // the references of the rows that outgrow theirs (of all, in the first step) move above the maximum of this step's scores; the
-          // others' stay, so that no row's numbers depend on another's
+          // others' stay, so that no row's numbers depend on another's.  A smaller lift moves all of them
 #pragma unroll 1
           for (int i = 0; i < mine; ++i) {
             uint64_t t[4];
@@ -723,15 +738,21 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
               if (lane == 0) *reinterpret_cast<float2*>(&sm.red_max[set][quad][8 * i + 2 * c]) = make_float2(m0, m1);
             }
           }
+          largest = warp_max(largest);
+          if (lane == 0) sm.red_scale[set][quad] = largest;
           if (j > 0 && quad == set) spin_for(&sm.o_done[b ^ 1], (g - 1) >> 1, abort_flag);                // O^T so far is complete
           set_sync(set);
+          largest = fmaxf(fmaxf(sm.red_scale[set][0], sm.red_scale[set][1]), fmaxf(sm.red_scale[set][2], sm.red_scale[set][3]));
+          const Lift now = started && largest <= lift.limit ? lift : lift_of(largest);
           if (quad == 0 && lane < 8 * mine) {
             const float m = fmaxf(fmaxf(sm.red_max[set][0][lane], sm.red_max[set][1][lane]), fmaxf(sm.red_max[set][2][lane], sm.red_max[set][3][lane]));
-            const float old = started ? -neg_ref[lane] : 0.f, top = m > -INFINITY ? m + kMargin : 0.f;
-            const float to = started && !(m - old > kGrow) ? old : top;
-            neg_ref[lane] = -to;
-            factor[lane] = to == old ? 1.f : fast_exp2(old - to);
+            const float old = started ? neg_ref[lane] : 0.f;
+            float to = now.orders - (m > -INFINITY ? m + kMargin : 0.f);
+            if (started && !(m + old - lift.orders > kGrow)) to = old + (now.orders - lift.orders);
+            neg_ref[lane] = to;
+            factor[lane] = to == old ? 1.f : fast_exp2(to - old);
           }
+          lift = now;
           set_sync(set);
           if (started) {
             fence_after_sync();

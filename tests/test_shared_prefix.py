@@ -201,6 +201,121 @@ def test_references_that_have_to_move(shape):
             assert np.abs(lse[a, h * rep:(h + 1) * rep] - want_lse).max() <= 1e-3
 
 
+def attended(f, a, h, s):
+    """Attention of query rows of KV head h over agent a's first keys, given the rows' scores: output, lse, and what its error is measured
+    in: the mean span of the values' groups (15 scales), the mean size of the values, the largest span."""
+    n = s.shape[1]
+    pos = np.arange(n)
+    _, V = O.gather_dequant(f.opool, 0, f.tables[a], 0, n, h)
+    span = 15.0 * np.repeat(O.sb_values(f.opool.Vs[0, f.tables[a][pos // 256], h, pos % 256]), 64, axis=-1)
+    top = s.max(1, keepdims=True)
+    p = np.exp(s - top)
+    l = p.sum(1, keepdims=True)
+    return p @ V / l, top[:, 0] + np.log(l[:, 0]), p @ span / l, p @ np.abs(V) / l, span.max()
+
+
+def code_bound(n, span, size, most):
+    """What the list may be off by, with one rounding of p s to binary16:
+      half a step, 2^-11 of p s, times a code of at most 15                                 -> 2^-11 * sum p span / sum p
+      scores of magnitude up to 20 from 16 sums of binary32 numbers, and an exponential     -> 1e-4 * sum p |v| / sum p
+      below binary16's range at most half of its smallest step 2^-24, sixteen times that for odd tokens, where the row's sum of p, lifted by
+      2^11 over the largest scale, is 2^10 over that scale or more: 15 * 2^-21 / 2^10 scales for a key, doubled -> n * 2^-30 * span."""
+    return 2.0 ** -11 * span + 1e-4 * size + n * 2.0 ** -30 * most
+
+
+N_SINK = 8192
+
+
+def behind_a_sink(shape, sharp, sigma, at, agents):
+    """Agents on one prefix in which key `at` is ten nats above the rest, which still have a good part of the weight together, and
+    values of size sigma: each probability by itself is small, and so is a value's scale."""
+    pos = np.arange(N_SINK)
+
+    def sink(f):
+        for t in (f.opool.Vs, f.opool.Vb):
+            t[:] = (t.astype(np.float32) * np.float32(sigma)).astype(np.float16)
+        for h in range(shape[1]):
+            where = (0, f.tables[0][pos // 256], h, pos % 256)
+            x = O.dequantize(O.unpack_codes(f.opool.Kc[where]), f.opool.Ks[where], f.opool.Kb[where]).astype(np.float32)
+            x[:, 0] = 0.0
+            x[at, 0] = 10.0 * math.sqrt(shape[2]) / (4.0 * sharp)
+            c, sc, b = O.quantize_rows(synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(x)))
+            f.opool.Kc[where], f.opool.Ks[where], f.opool.Kb[where] = O.pack_codes(c), sc, b
+
+    f = Forked(shape, [(N_SINK, [0] * agents)], seed=45, edit=sink, wide=WIDE)
+    qf = synth.bf16_bits_to_f32(f.q()) * np.float32(0.5 / sharp)
+    qf[..., 0] = 4.0
+    return f, synth.f32_to_bf16_bits(qf), sharp / math.sqrt(shape[2])
+
+
+def close_behind_a_sink(f, q, scale, at, out, lse, codes):
+    """codes: the route multiplies the codes; else it expands keys and values into binary16 tiles, which costs every key element a
+    rounding of 2^-11 at most, a score d = 2^-11 * scale * sum |q k| at most, a weight 2 d of itself; and 2^-11 each for values and
+    probabilities."""
+    shape = f.shape
+    qd, rep = synth.bf16_bits_to_f32(q).astype(np.float64), shape[0] // shape[1]
+    for h in range(shape[1]):
+        heads = slice(h * rep, (h + 1) * rep)
+        K, V = O.gather_dequant(f.opool, 0, f.tables[0], 0, N_SINK, h)
+        rows = qd[:, heads].reshape(-1, shape[2])
+        s = scale * rows @ K.T
+        want, want_lse, *sizes = attended(f, 0, h, s)
+        assert 0.3 < np.exp(s[:, at] - want_lse).mean() < 0.97           # the sink has much of the weight, and so have the others
+        err = np.abs(out[:, heads].double().cpu().numpy().reshape(-1, shape[3]) - want)
+        off = np.abs(lse[:, heads].double().cpu().numpy().reshape(-1) - want_lse)
+        assert np.all(err.max(1) <= RTOL_ROW * np.abs(want).max(1)), (err.max(1) / np.abs(want).max(1)).max()
+        d = 2.0 ** -11 * scale * (np.abs(rows) @ np.abs(K).T).max(1)
+        if codes:
+            assert np.all(err <= code_bound(N_SINK, *sizes)) and off.max() <= 2e-3
+        else:
+            assert np.all(err <= (2.0 ** -10 + 2.1 * d[:, None]) * np.abs(V).max()) and np.all(off <= d + 1e-3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at", [0, 1, 5003])
+@pytest.mark.parametrize("sigma", [1.0, 0.1, 0.05, 0.01])
+@pytest.mark.parametrize("sharp", [1.0, 2.5])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
+def test_keys_behind_a_sink_keep_their_values(shape, sharp, sigma, at):
+    """152 agents, so that a CTA of the list has some 2000 keys.  The larger scale does not go to tiles."""
+    f, q, scale = behind_a_sink(shape, sharp, sigma, at, 152)
+    out, lse = f.run(q, scale)
+    assert f.dc.read_flags() == 0
+    close_behind_a_sink(f, q, scale, at, out, lse, codes=sharp > 2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sb_dtype", [0, 1])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
+def test_values_whose_size_changes_along_the_prefix(shape, sb_dtype):
+    """Value scales that climb and fall by sixteen binary orders within 1024 keys, and groups that are all one number (scale 0)."""
+    n = 8192
+    pos = np.arange(n)
+
+    def climb(f):
+        for h in range(shape[1]):
+            where = (0, f.tables[0][pos // 256], h, pos % 256)
+            x = O.dequantize(O.unpack_codes(f.opool.Vc[where]), f.opool.Vs[where], f.opool.Vb[where]).astype(np.float32)
+            x *= (2.0 ** (np.abs(pos % 1024 - 512) / 32.0 - 10.0))[:, None].astype(np.float32)
+            x[pos % 7 == 3, :64] = 0.375
+            x[:200] = 0.375
+            c, sc, b = O.quantize_rows(synth.bf16_bits_to_f32(synth.f32_to_bf16_bits(x)), sb_dtype)
+            f.opool.Vc[where], f.opool.Vs[where], f.opool.Vb[where] = O.pack_codes(c), sc, b
+
+    f = Forked(shape, [(n, [0] * 152)], seed=46, sb_dtype=sb_dtype, edit=climb, wide=WIDE)
+    q, scale = f.q(), 2.5 / math.sqrt(shape[2])          # not by tiles
+    out, lse = f.run(q, scale)
+    assert f.dc.read_flags() == 0
+    qd, rep = synth.bf16_bits_to_f32(q).astype(np.float64), shape[0] // shape[1]
+    for h in range(shape[1]):
+        heads = slice(h * rep, (h + 1) * rep)
+        K, _ = O.gather_dequant(f.opool, 0, f.tables[0], 0, n, h)
+        want, want_lse, *sizes = attended(f, 0, h, scale * qd[:, heads].reshape(-1, shape[2]) @ K.T)
+        err = np.abs(out[:, heads].double().cpu().numpy().reshape(-1, shape[3]) - want)
+        assert np.all(err <= code_bound(n, *sizes))
+        assert np.abs(lse[:, heads].double().cpu().numpy().reshape(-1) - want_lse).max() <= 2e-3
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape, agents", [((4, 2, 128, 128), 4), ((4, 4, 192, 128), 8), ((4, 2, 256, 256), 3)])
 def test_groups_of_at_most_eight_rows(shape, agents):
