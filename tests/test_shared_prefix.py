@@ -285,6 +285,20 @@ def test_keys_behind_a_sink_keep_their_values(shape, sharp, sigma, at):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("at", [0, 1, 5003])
+@pytest.mark.parametrize("sigma", [1.0, 0.1, 0.05, 0.01])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (16, 2, 128, 128), (3, 3, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
+def test_agents_by_themselves_keep_values_behind_a_sink(shape, sigma, at):
+    """The same keys, attended by every agent alone: in this call and in the decode call."""
+    f, q, scale = behind_a_sink(shape, 1.0, sigma, at, 40)
+    out, lse = f.dc.shared_prefix_decode(0, f.lens, list(range(41)), [N_SINK] * 40, q, scale)
+    close_behind_a_sink(f, q, scale, at, out, lse, codes=True)
+    out, lse = f.dc.decode(0, f.lens, 0, q, scale)
+    close_behind_a_sink(f, q, scale, at, out, lse, codes=True)
+    assert f.dc.read_flags() == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("sb_dtype", [0, 1])
 @pytest.mark.parametrize("shape", [(8, 2, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
 def test_values_whose_size_changes_along_the_prefix(shape, sb_dtype):
