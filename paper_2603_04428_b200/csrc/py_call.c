@@ -26,11 +26,12 @@ static int (*f_copy_blocks)(const q4kv_spec*, const void*, int32_t, void*, int32
                             int32_t*, void*);
 static int (*f_shared_prefix)(const q4kv_spec*, const void*, int32_t, int32_t, const q4kv_batch*, const int32_t*, int32_t, const int32_t*,
                               const int32_t*, int32_t, const void*, float, void*, int32_t, float*, void*, size_t, int32_t*, void*);
-static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes, *s_get_device, *s_stride, *s_element_size;
+static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_nbytes, *s_get_device, *s_stride, *s_dtype, *s_shape;
+static PyObject* bfloat16;                                 /* torch.bfloat16 */
 
-/* A device pointer: None, an integer, or a contiguous CUDA tensor. */
 static int on_device(PyObject* o, long dev);
-/* dev: the device that a tensor has to lie on (which also says that it is a CUDA tensor), or kAnyDevice */
+/* A device pointer: None, an integer, or a contiguous CUDA tensor.
+   dev: the device that a tensor has to lie on (which also says that it is a CUDA tensor), or kAnyDevice */
 enum { kAnyDevice = -1 };
 static int get_ptr_at(PyObject* o, long dev, void** out) {
   if (o == Py_None) { *out = NULL; return 1; }
@@ -162,7 +163,7 @@ static PyObject* prefill(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
 }
-/* The same as get_ptr for a tensor that has to lie on device dev (an integer or None is taken as it is). */
+/* Whether a tensor lies on device dev (an integer or None does). */
 static int on_device(PyObject* o, long dev) {
   if (o == Py_None || PyLong_Check(o)) return 1;
   PyObject* r = PyObject_CallMethodNoArgs(o, s_get_device);
@@ -173,11 +174,32 @@ static int on_device(PyObject* o, long dev) {
   if (at != dev) { PyErr_SetString(PyExc_AssertionError, "a tensor lies on another device than the current one"); return 0; }
   return 1;
 }
+/* The same as get_ptr for a tensor that has to lie on device dev. */
 static int get_ptr_on(PyObject* o, int32_t dev, void** out) {
   if (dev < 0) { PyErr_SetString(PyExc_AssertionError, "no such device"); return 0; }
   return get_ptr_at(o, dev, out);
 }
-/* Rows [tokens][heads][d] of 16-bit elements whose first stride is free: pointer and stride. */
+static int is_bf16(PyObject* o) {                          /* -1: an error is set */
+  PyObject* r = PyObject_GetAttr(o, s_dtype);
+  if (!r) return -1;
+  const int same = r == bfloat16;
+  Py_DECREF(r);
+  return same;
+}
+/* Whether the shape is [at least rows][heads][d] (no len(): it takes a tensor longer than all the rest of these calls). */
+static int has_shape(PyObject* o, int64_t rows, int64_t heads, int64_t d) {
+  PyObject* r = PyObject_GetAttr(o, s_shape);
+  if (!r) { PyErr_Clear(); return 0; }
+  int ok = PyTuple_Check(r) && PyTuple_GET_SIZE(r) == 3;
+  const int64_t want[3] = {rows, heads, d};
+  for (int i = 0; ok && i < 3; ++i) {
+    const int64_t n = PyLong_AsLongLong(PyTuple_GET_ITEM(r, i));
+    ok = i == 0 ? n >= want[i] : n == want[i];
+  }
+  Py_DECREF(r);
+  return ok;
+}
+/* Rows [tokens][heads][d] of bfloat16 whose first stride is free: pointer and stride. */
 static int get_rows(PyObject* o, long dev, void** out, int64_t heads, int64_t d, int64_t rows, int64_t* stride) {
   int64_t st[3];
   PyObject* r;
@@ -187,13 +209,9 @@ static int get_rows(PyObject* o, long dev, void** out, int64_t heads, int64_t d,
   int ok = PyArg_ParseTuple(r, "LLL", &st[0], &st[1], &st[2]);
   Py_DECREF(r);
   if (!ok) return 0;
-  if (!(r = PyObject_CallMethodNoArgs(o, s_element_size))) return 0;
-  ok = PyLong_AsLong(r) == 2;
-  Py_DECREF(r);
+  ok = rows <= 0 || (has_shape(o, rows, heads, d) && (st[2] == 1 || d == 1) && (st[1] == d || heads == 1) && is_bf16(o) != 0);
   if (PyErr_Occurred()) return 0;
-  const Py_ssize_t n = PyObject_Length(o);
-  if (n < 0) return 0;
-  if (!ok || (n > 0 && rows > 0 && (n < rows || (st[2] != 1 && d > 1) || (st[1] != d && heads > 1)))) {
+  if (!ok) {
     PyErr_SetString(PyExc_AssertionError, "rows are bfloat16 [tokens][heads][d] with whole heads next to each other");
     return 0;
   }
@@ -202,6 +220,19 @@ static int get_rows(PyObject* o, long dev, void** out, int64_t heads, int64_t d,
   *out = PyLong_AsVoidPtr(r);
   Py_DECREF(r);
   return !(*out == NULL && PyErr_Occurred());
+}
+/* Where such rows go: a contiguous bfloat16 tensor with room for them, whatever its shape. */
+static int get_rows_out(PyObject* o, int32_t dev, void** out, int64_t heads, int64_t d, int64_t rows) {
+  size_t bytes;
+  if (!get_ptr_on(o, dev, out)) return 0;
+  if (o == Py_None || PyLong_Check(o) || rows <= 0) return 1;
+  const int ok = is_bf16(o);
+  if (ok < 0 || !get_bytes(o, &bytes)) return 0;
+  if (!ok || bytes / 2 / (size_t)rows < (size_t)(heads * d)) {
+    PyErr_SetString(PyExc_AssertionError, "an output is bfloat16 with room for every row");
+    return 0;
+  }
+  return 1;
 }
 /* spec, how, n_agents, pos, new_offs, total_new, q, k, q_out, k_out, status_flags, stream, device */
 static PyObject* norm_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -214,8 +245,9 @@ static PyObject* norm_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   if (!count(n, 13) || !get_struct(a[0], &spec, sizeof spec) || !get_struct(a[1], &how, sizeof how) || !get_i32(a[2], &agents) ||
       !get_i32(a[12], &dev) || !get_ptr_on(a[3], dev, &pos) || !get_ptr_on(a[4], dev, &offs) || !get_i32(a[5], &total) ||
       !get_rows(a[6], dev, &q, spec.n_q_heads, spec.d_qk, total, &qs) ||
-      !get_rows(a[7], dev, &k, spec.n_kv_heads, spec.d_qk, total, &ks) || !get_ptr_on(a[8], dev, &qo) ||
-      !get_ptr_on(a[9], dev, &ko) || !get_ptr_on(a[10], dev, &flags) || !get_ptr(a[11], &stream))
+      !get_rows(a[7], dev, &k, spec.n_kv_heads, spec.d_qk, total, &ks) ||
+      !get_rows_out(a[8], dev, &qo, spec.n_q_heads, spec.d_qk, total) ||
+      !get_rows_out(a[9], dev, &ko, spec.n_kv_heads, spec.d_qk, total) || !get_ptr_on(a[10], dev, &flags) || !get_ptr(a[11], &stream))
     return NULL;
   Py_BEGIN_ALLOW_THREADS
   rc = f_norm_rope(&spec, &how, agents, pos, offs, total, q, qs, k, ks, qo, ko, flags, stream);
@@ -279,6 +311,12 @@ PyMODINIT_FUNC PyInit__call(void) {
   s_nbytes = PyUnicode_InternFromString("nbytes");
   s_get_device = PyUnicode_InternFromString("get_device");
   s_stride = PyUnicode_InternFromString("stride");
-  s_element_size = PyUnicode_InternFromString("element_size");
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_shape = PyUnicode_InternFromString("shape");
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return NULL;
+  bfloat16 = PyObject_GetAttrString(torch, "bfloat16");
+  Py_DECREF(torch);
+  if (!bfloat16) return NULL;
   return PyModule_Create(&module);
 }

@@ -274,3 +274,66 @@ def _call_on(device, spec, how):
         B.q4kv_norm_rope(spec, how, 1, 0x1000, 0x1000, 0, None, None, None, None)
     finally:
         B._device = keep
+
+
+class _Rows:
+    """Looks like a CUDA tensor [tokens][heads][d] on device 0."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype=torch.bfloat16, stride=None):
+        self.shape, self.dtype, self._t = torch.Size(shape), dtype, torch.empty(shape, dtype=dtype, device="meta")
+        self.nbytes, self._stride = self._t.nbytes, stride or self._t.stride()
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return id(self) & ~0xFFFF
+
+    def get_device(self):
+        return 0
+
+    def stride(self):
+        return self._stride
+
+    def element_size(self):
+        return self._t.element_size()
+
+    def __len__(self):
+        return self.shape[0]
+
+
+def test_tensors_of_other_sizes_and_types_are_refused():
+    if torch.cuda.is_available():
+        pytest.skip("placeholder pointers are only handed to the library on a host without a CUDA device")
+    call, spec, how = B._native(), B.Spec.make(1, 8, 2, 128, 128), B.NormRotation()
+
+    def norm_rope(q=None, k=None, q_out=None, k_out=None, total=4):
+        q, k = q or _Rows((4, 8, 128)), k or _Rows((4, 2, 128))
+        q_out, k_out = q_out or _Rows((4, 8, 128)), k_out or _Rows((4, 2, 128))
+        return call.norm_rope(spec, how, 0, 0x1000, 0x1000, total, q, k, q_out, k_out, None, None, 0)     # no agents: nothing is launched
+
+    assert norm_rope() == norm_rope(q=_Rows((4, 8, 128), stride=(1536, 128, 1))) == norm_rope(q_out=_Rows((4, 1024, 1))) == B.OK
+    assert norm_rope(total=3) == norm_rope(q=_Rows((9, 8, 128)), k_out=_Rows((5, 2, 128))) == B.OK
+    for bad in (dict(q=_Rows((4, 8, 128), torch.float16)), dict(q=_Rows((4, 8, 128), torch.float32)), dict(k=_Rows((4, 2, 128), torch.int16)),
+                dict(q=_Rows((4, 2, 128))), dict(k=_Rows((4, 1, 128))), dict(q=_Rows((4, 9, 128))), dict(q=_Rows((4, 8, 64), stride=(1024, 128, 1))),
+                dict(q=_Rows((3, 8, 128))), dict(k=_Rows((4, 2, 128), stride=(512, 256, 1)))):
+        with pytest.raises(AssertionError, match="rows are"):
+            norm_rope(**bad)
+    for bad in (dict(q_out=_Rows((3, 8, 128))), dict(k_out=_Rows((4, 2, 64))), dict(q_out=_Rows((4, 2, 128))),
+                dict(q_out=_Rows((4, 8, 128), torch.float16)), dict(k_out=_Rows((4, 2, 128), torch.float32))):
+        with pytest.raises(AssertionError, match="an output is"):
+            norm_rope(**bad)
+
+
+@pytest.mark.gpu
+def test_rows_of_other_heads_and_types_are_refused_on_the_device():
+    f = torch.from_numpy(theta(128)).cuda()
+    spec, how = B.Spec.make(1, 8, 2, 128, 128), B.NormRotation.make(rot_dim=128, inv_freq=f)
+    x = torch.zeros((4, 12, 128), dtype=torch.bfloat16, device="cuda")
+    pos, offs = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    out = torch.empty((4, 8, 128), dtype=torch.bfloat16, device="cuda")
+    B.q4kv_norm_rope(spec, how, 1, pos, offs, 4, x[:, :8], None, out, None)
+    for q, o in ((x[:, 8:10], out), (x[:, :8].half(), out), (x[:, :8, :64], out), (x[:, :8], out[:3]), (x[:, :8], out.float())):
+        with pytest.raises(AssertionError):
+            B.q4kv_norm_rope(spec, how, 1, pos, offs, 4, q, None, o, None)
