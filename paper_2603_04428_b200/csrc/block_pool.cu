@@ -112,7 +112,7 @@ int32_t q4kv_allocator_agent_blocks(const q4kv_allocator* al, int64_t agent_id) 
 
 int q4kv_allocator_reserve(q4kv_allocator* al, int64_t agent_id, int32_t n_tokens, int32_t* table_row, int32_t max_blocks) {
   if (!al || n_tokens < 0 || !table_row || max_blocks <= 0) return Q4KV_EINVAL;
-  const int32_t want = (n_tokens + kBlockTokens - 1) / kBlockTokens;
+  const int32_t want = n_tokens / kBlockTokens + (n_tokens % kBlockTokens ? 1 : 0);
   if (want > max_blocks) return Q4KV_EINVAL;
   auto it = al->agents.find(agent_id);
   const int32_t have = it == al->agents.end() ? 0 : (int32_t)it->second.blocks.size();

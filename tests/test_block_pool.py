@@ -76,3 +76,14 @@ def test_oracle_dense_batch_is_left_padded_and_merge_inverts_extract():
     O.merge_dense(pool2, 1, tabs2, lens, T, dense)
     assert np.array_equal(O.extract_dense(pool2, 1, tabs2, lens, T), dense)
     assert np.all(pool2.Kc[0] == 0)                                                  # the other layer is untouched
+
+
+def test_a_reservation_beyond_every_row_is_refused():
+    al = B.Allocator(4)
+    al.reserve(1, 300, 4)
+    for n in (2**31 - 1, 2**31 - 255, 2**31 - 256, 4 * 256 + 1):
+        for agent in (1, 2):
+            with pytest.raises(B.Q4KVError) as e:
+                al.reserve(agent, n, 4)
+            assert e.value.code == B.EINVAL
+    assert al.agent_blocks(1) == 2 and al.agent_blocks(2) == 0 and al.free_blocks() == 2
