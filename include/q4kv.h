@@ -433,7 +433,8 @@ void q4kv_allocator_destroy(q4kv_allocator* allocator);
 int32_t q4kv_allocator_free_blocks(const q4kv_allocator* allocator);
 int32_t q4kv_allocator_agent_blocks(const q4kv_allocator* allocator, int64_t agent_id);   /* 0: unknown agent */
 /* Make the agent's block list cover n_tokens (it only grows; earlier blocks keep their place), mark the agent most
- * recently used, and write its block-table row to table_row (HOST, max_blocks entries, -1 past the last block). */
+ * recently used, and write its block-table row to table_row (HOST, max_blocks entries, -1 past the last block).
+ * EWORKSPACE: too few free blocks (or no host memory), and nothing has changed. */
 int q4kv_allocator_reserve(q4kv_allocator* allocator, int64_t agent_id, int32_t n_tokens, int32_t* table_row,
                            int32_t max_blocks);
 int q4kv_allocator_touch(q4kv_allocator* allocator, int64_t agent_id);                    /* most recently used */

@@ -117,12 +117,21 @@ int q4kv_allocator_reserve(q4kv_allocator* al, int64_t agent_id, int32_t n_token
   auto it = al->agents.find(agent_id);
   const int32_t have = it == al->agents.end() ? 0 : (int32_t)it->second.blocks.size();
   if (want > have && (size_t)(want - have) > al->free_list.size()) return Q4KV_EWORKSPACE;   // evict first (pick a victim)
-  if (it == al->agents.end()) {
-    it = al->agents.emplace(agent_id, q4kv_allocator::Agent()).first;
-    al->lru.push_back(agent_id);
-    it->second.lru_pos = std::prev(al->lru.end());
-  } else {
-    touch(al, it->second);
+  try {                                                // everything that can fail comes before the first change
+    if (it == al->agents.end()) {
+      q4kv_allocator::Agent fresh;
+      fresh.blocks.reserve(want);
+      std::list<int64_t> node(1, agent_id);
+      it = al->agents.emplace(agent_id, std::move(fresh)).first;
+      al->lru.splice(al->lru.end(), node);
+      it->second.lru_pos = std::prev(al->lru.end());
+    } else {
+      std::vector<int32_t>& blocks = it->second.blocks;
+      if ((size_t)want > blocks.capacity()) blocks.reserve(std::max((size_t)want, std::min(2 * blocks.capacity(), (size_t)al->n_blocks)));
+      touch(al, it->second);
+    }
+  } catch (...) {                                      // no host memory
+    return Q4KV_EWORKSPACE;
   }
   q4kv_allocator::Agent& ag = it->second;
   while ((int32_t)ag.blocks.size() < want) ag.blocks.push_back(take_block(al));

@@ -1,10 +1,16 @@
 """Host-side block bookkeeping (Section 3.1: per-agent isolation, LRU eviction) and the oracle's dense-batch
 functions (Section 3.4: merge / extract).  No kernel is launched here."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
 from oracle import q4kv_oracle as O
 from paper_2603_04428_b200 import binding as B, synth
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def test_blocks_are_exclusive_grow_in_place_and_come_back_on_release():
@@ -87,3 +93,28 @@ def test_a_reservation_beyond_every_row_is_refused():
                 al.reserve(agent, n, 4)
             assert e.value.code == B.EINVAL
     assert al.agent_blocks(1) == 2 and al.agent_blocks(2) == 0 and al.free_blocks() == 2
+
+
+_NO_MEMORY = """
+import ctypes, resource
+from paper_2603_04428_b200 import binding as B
+lib, n = B.lib(), 1 << 22
+al = B.Allocator(n)
+row, copy = (ctypes.c_int32 * n)(), (ctypes.c_int32 * 3)()
+assert lib.q4kv_allocator_reserve(al._h, 1, 2560, row, n) == B.OK
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+before = resource.getrlimit(resource.RLIMIT_AS)
+resource.setrlimit(resource.RLIMIT_AS, (used + (2 << 20), before[1]))
+codes = [lib.q4kv_allocator_reserve(al._h, agent, 256 * (n - 20), row, n) for agent in (1, 2)]       # a list of 16 MB
+resource.setrlimit(resource.RLIMIT_AS, before)
+assert codes == [B.EWORKSPACE] * 2, codes
+assert al.free_blocks() == n - 10 and al.agent_blocks(1) == 10 and al.agent_blocks(2) == 0 and al.pick_victim() == 1
+assert sum(al.block_holders(b) for b in range(n)) == 10
+assert lib.q4kv_allocator_reserve(al._h, 2, 256 * (n - 20), row, n) == B.OK and al.free_blocks() == 10
+print("done")
+"""
+
+
+def test_a_reservation_without_host_memory_changes_nothing():
+    done = subprocess.run([sys.executable, "-c", _NO_MEMORY], capture_output=True, text=True, cwd=ROOT, timeout=300)
+    assert done.returncode == 0 and "done" in done.stdout, done.stderr
