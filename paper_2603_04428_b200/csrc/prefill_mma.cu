@@ -20,8 +20,8 @@
 //     part is a per-row float32 scalar sum.
 //   * The score fragment of two adjacent key tiles is the A fragment of the value product, as in any
 //     register-resident flash attention, so probabilities never leave their lane.
-// Measured: 146 TFLOP/s on 8 x (8192 + 1024) tokens at d = 128 with 32 / 8 heads; 148 TFLOP/s on 8 x (4096 + 512)
-// tokens at d = 256 with 16 / 8 heads.
+// Measured: 141 TFLOP/s on 8 x (8192 + 1024) tokens at d = 128 with 32 / 8 heads; 143 TFLOP/s on 8 x (4096 + 512)
+// tokens at d = 256 with 16 / 8 heads (146 and 147 with probabilities of at most 1, which lose small ones' values).
 #include "convert.cuh"
 #include "q4kv_layout.cuh"
 #include "quantize_core.cuh"
@@ -213,6 +213,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
     for (int nt = 0; nt < Dv / 8; ++nt) { o[rt][nt][0] = 0.f; o[rt][nt][1] = 0.f; o[rt][nt][2] = 0.f; o[rt][nt][3] = 0.f; }
   }
   bool aborted = false, poisoned = false;
+  float room = 40.f;                                     // binary orders, see below
+  uint32_t vlimit = 0u;                                  // the largest value scale (bit pattern) that leaves it
   const int W = P.window;
 
   for (int k = 0; k < n_chunks; ++k) {
@@ -228,6 +230,39 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
       const uint4* vsb4 = reinterpret_cast<const uint4*>(chunk + 32 * (D / 2) + 128 * G + 32 * (Dv / 2));
       const int pos0 = (c_begin + k) * 32;
       const bool tail = pos0 + 32 > kv_len;              // slots past the cache end may hold stale bytes
+
+      // Probabilities are as many binary orders above 1 as the value scales seen so far allow (p * s_v below 2^15): both terms of the
+      // binary16 sum lose what falls below 2^-24, sixteen times as much in the odd tiles, while the bias sums lose nothing, so that
+      // a key with a small probability would count as its group's minimum.
+      uint32_t vmax;
+      if (G == 2) {
+        const uint2 v = reinterpret_cast<const uint2*>(vsb4)[lane];
+        vmax = __vmaxu2(v.x, v.y) & 0xFFFFu;
+      } else {
+        const uint4 v = vsb4[lane];
+        vmax = __vmaxu2(__vmaxu2(v.x, v.y), __vmaxu2(v.z, v.w)) & 0xFFFFu;
+      }
+      if (tail && pos0 + 8 * ((lane >> 1) & 3) + 4 * (lane & 1) + (lane >> 3) >= kv_len) vmax = 0u;       // see sb_offset
+      vmax = __reduce_max_sync(0xffffffffu, vmax);
+      if (vmax > vlimit) {
+        // scales below 2^(e + 1), twice what there is or more, leave 13 - e binary orders
+        const uint32_t v = min(vmax, 0x7FFFu);           // a negative scale: no room
+        const int e = kBf ? (int)(v >> 7) - 126 : (int)(v >> 10) - 14;
+        const float to = fminf(room, (float)(13 - max(e, -26))), f = fast_exp2(to - room);
+        vlimit = vmax > 0x7FFFu ? 0xFFFFu : (v | (kBf ? 0x7Fu : 0x3FFu)) + (kBf ? 0x80u : 0x400u);
+        room = to;
+#pragma unroll
+        for (int rt = 0; rt < R; ++rt) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            l_e[rt][r] *= f; l_o[rt][r] *= f;
+#pragma unroll
+            for (int gi = 0; gi < G; ++gi) { bias_e[rt][r][gi] *= f; bias_o[rt][r][gi] *= f; }
+          }
+#pragma unroll
+          for (int nt = 0; nt < Dv / 8; ++nt) { o[rt][nt][0] *= f; o[rt][nt][1] *= f; o[rt][nt][2] *= f; o[rt][nt][3] *= f; }
+        }
+      }
 
       // Two forms of the same step.  d = 128 (two 16-row tiles per warp): all groups' operands of the value product
       // are built first.  d = 256 (one tile per warp, 128 accumulator registers per lane): keys and values are taken
@@ -303,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
             m_run[rt][r] = m_new;
   #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float off = (i & 1) ? m_new + 4.f : m_new;   // odd tiles: p / 16 (their value codes carry a factor 16)
+              const float off = (i & 1) ? m_new + (4.f - room) : m_new - room;   // odd tiles: p / 16 (their value codes carry a factor 16)
               s[i][0][r] = fast_exp2(s[i][0][r] - off);
               s[i][1][r] = fast_exp2(s[i][1][r] - off);
             }
@@ -465,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
             m_run[rt][r] = m_new;
   #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float off = (i & 1) ? m_new + 4.f : m_new;   // odd tiles: p / 16 (their value codes carry a factor 16)
+              const float off = (i & 1) ? m_new + (4.f - room) : m_new - room;   // odd tiles: p / 16 (their value codes carry a factor 16)
               sc[i][0][r] = fast_exp2(sc[i][0][r] - off);
               sc[i][1][r] = fast_exp2(sc[i][1][r] - off);
             }
@@ -600,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_mma_kernel(const __grid_c
           *reinterpret_cast<float2*>(reinterpret_cast<float*>(P.out) + row * Dv + d) = make_float2(v0, v1);
         }
       }
-      if (tid == 0 && P.lse) P.lse[row] = l > 0.f ? (m_run[rt][r] + log2f(l)) / kLog2e : -INFINITY;
+      if (tid == 0 && P.lse) P.lse[row] = l > 0.f ? (m_run[rt][r] - room + log2f(l)) / kLog2e : -INFINITY;
     }
 }
 

@@ -299,6 +299,18 @@ def test_agents_by_themselves_keep_values_behind_a_sink(shape, sigma, at):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("at", [0, 1, 5003])
+@pytest.mark.parametrize("sigma", [1.0, 0.1, 0.01])
+@pytest.mark.parametrize("shape", [(8, 2, 128, 128), (3, 3, 128, 128), (4, 2, 256, 256)])
+def test_exact_prefill_keeps_values_behind_a_sink(shape, sigma, at):
+    """The same keys in the prefill kernel that multiplies codes (its queries being the last token of each agent)."""
+    f, q, scale = behind_a_sink(shape, 2.5, sigma, at, 5)
+    out, lse = f.dc.prefill(0, f.lens, list(range(6)), 0, q, scale)
+    assert f.dc.read_flags() == 0
+    close_behind_a_sink(f, q, scale, at, out, lse, codes=True)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("sb_dtype", [0, 1])
 @pytest.mark.parametrize("shape", [(8, 2, 128, 128), (8, 2, 192, 128), (4, 2, 256, 256)])
 def test_values_whose_size_changes_along_the_prefix(shape, sb_dtype):
