@@ -117,9 +117,13 @@ enum { Q4KV_OUT_F32 = 0, Q4KV_OUT_BF16 = 1 };
  *     below is not allowed; prefill with d in {128, 256} when it is not; the shape-agnostic kernels
  *     every other case falls back to): the products are exact, sums are float32, the
  *     probabilities enter the value product as a two-term binary16 pair or as float32.  Error
- *     at most 2e-5 * M + 1e-5, i.e. within 2e-3 for any cache with M <= 64.  (An absolute bound:
- *     the tensor-core kernels carry probability x scale in binary16, so contributions of groups
- *     whose scale is below 2^-24 vanish; only bfloat16 caches can hold such scales.)
+ *     at most 2e-5 * M + 1e-5, i.e. within 2e-3 for any cache with M <= 64; in prefill with d in
+ *     {128, 256}, where one warp adds up all n keys of a row in the tensor cores, which truncate,
+ *     n * 2^-25 * M more at most (measured 5e-4 at n = 8192, M = 11, one early key with most of the
+ *     weight).  (An absolute bound: the tensor-core kernels carry probability x scale in binary16,
+ *     decode and prefill with as many binary orders to spare as the value scales allow, so that
+ *     contributions below 2^-30 of the largest may vanish; on the latent cache, those of groups
+ *     whose scale is below 2^-24, which only bfloat16 caches can hold.)
  *   - Kernels that expand the cache into binary16 tiles (prefill with d_qk = d_v in {128, 256}, d_qk 192 / d_v 128 or, V
  *     aliasing K, d_qk 576 / d_v 512; decode on the MLA-latent cache: V aliasing K, d_qk 576, d_v 512, one
  *     KV head, at most 16 query heads) round every dequantized value once to binary16, a relative
@@ -248,8 +252,8 @@ int q4kv_decode_attention_layers(const q4kv_spec* spec, void* pool, int32_t n_bl
  *                is an agent without tokens of its own; kv_len == 0 gives zeros and lse = -inf without a flag.  A length below
  *                its group's prefix, negative or above max_kv_len, a bad prefix length, an agent outside every group, or offsets
  *                that do not ascend raise Q4KV_FLAG_BAD_LENGTH and give zeros for the agents concerned.
- *   max_kv_len   as for q4kv_decode_attention; which way a call takes is estimated from it, n_agents and n_groups, so a bound near
- *                the lengths serves best
+ *   max_kv_len   as for q4kv_decode_attention; which way a call takes is estimated from it, n_agents and n_groups as if the groups
+ *                were alike, so a bound near the lengths serves best
  *   workspace    at least q4kv_workspace_bytes_shared_prefix bytes, its header zeroed once as for q4kv_decode_attention, which may
  *                share it.  One made for the most agents, groups and the longest context serves smaller calls
  * Like the other lengths, group_offs and prefix_lens are read before the preceding kernels of the stream have completed.

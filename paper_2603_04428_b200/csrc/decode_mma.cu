@@ -40,7 +40,8 @@
 //     d = 128) that are attended like KV heads of their own and read the chunks again, from L2 for the most part.
 // Measured per launch in a replayed step (before: the form with seven consumer warps and a planner): d = 128, 4 heads per
 // KV head, 8 KV heads, agents x 4096 tokens: 1 agent 14.1 -> 8.9 us, 5 agents 17.5 -> 11.8 us (2.0 TB/s), 40 agents 72.9
-// -> 49.8 us (3.8 TB/s); d = 256, 16 agents x 8192 tokens, 81.4 -> 72.1 us (4.2 TB/s); 8 query heads per KV head, 12 agents
+// -> 49.8 us (3.8 TB/s); d = 256, 16 agents x 8192 tokens, 81.4 -> 72.1 us (4.2 TB/s; 2 % more with
+// the room that chunk_values leaves the probabilities); 8 query heads per KV head, 12 agents
 // x 4096 tokens: 26 us with the append, 1.5 ms on the shape-agnostic kernel.
 //   * The reference of a warp's online softmax is taken over the warp, and the accumulators are rescaled, only when one
 //     vote says that some score outgrew it by a binary order, or a value scale the room that was left for it.
@@ -289,10 +290,10 @@ __device__ inline RangeStart find_range(const Par& P, int cta, int grid, uint32_
     const unsigned fits = __ballot_sync(0xffffffffu, total * Hkv <= (int)most && lane <= kWholeSlack);
     // A pair whole in one CTA needs no records and no ticket (2 us).  That is worth a round of chunks, one per warp, where the pairs are
     // few, and a seventh of the rounds where there are many.  Measured, us a launch, cut and whole: eight heads, 16 x 700 tokens
-    // 15.0 / 15.9; d = 256, one x 350 9.0 / 9.9, 20 agents in a window of 1024 27.0 / 26.2.  Up to four heads at d = 128 stay cut all
-    // the same: terms of p * s below 2^-24 are cut off against the reference of all the chunks that a warp adds up, and twice the
-    // chunks lose more.  Error against 64 bits (relative, outlier channels), cut and whole, 8 KV heads: one agent x 480 tokens 1.44e-4 /
-    // 1.95e-4 (6.5 / 5.8 us), 32 x 4096 8.5e-4 / 10.6e-4 (39.4 / 35.9 us); d = 256, 20 in a window 3.13e-4 / 3.13e-4.
+    // 15.0 / 15.9; d = 256, one x 350 9.0 / 9.9, 20 agents in a window of 1024 27.0 / 26.2.  Up to four heads at d = 128 stay cut:
+    // that was for small terms of p * s, of which twice the chunks lost more; since the probabilities have room above 1 (chunk_values)
+    // neither form loses them.  Error against 64 bits (outlier channels), cut and whole, 8 KV heads: one agent x 480 tokens 5.9e-5 /
+    // 5.8e-5 (5.9 / 5.3 us), 32 x 4096 5.7e-5 / 6.0e-5 (37.8 / 34.8 us).
     const int l = fits ? __ffs(fits) - 1 : 0, pairs = n_agents * Hkv;
     const int rounds = (size0 + l + (int)nw - 1) / (int)nw;
     const int extra = more_rounds < 0 ? 0 : (rounds * 37 >> 8) + (more_rounds == 1 || 4 * pairs <= (int)most ? min(more_rounds, 1) : 0);

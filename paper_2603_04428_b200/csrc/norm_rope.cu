@@ -5,11 +5,12 @@
 //   (y_a, y_b) -> scale * (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position * inv_freq[j]
 //
 // Every element is read once and written once (bound: HBM), a handful of binary32 operations each, rounded once to bfloat16
-// (between the norm and the rotation nothing is rounded).  The angles are the expensive part: position * inv_freq is exact in
-// binary64 (31 + 24 bits at most, rounded at 53), and reduced there, because in binary32 an angle of 10^5 is off by 4e-3.  All
-// heads of a token share its angles, and what norm weights and angles make of an element's two factors: a warp takes one token (or a
-// part of its heads, when there are few tokens), turns rot_dim / 2 angles into cosines and sines in its part of shared memory and keeps
-// the factors of its elements in registers for all of its heads.  Warps never wait for one another.
+// (between the norm and the rotation nothing is rounded).  The angles are the expensive part: they are taken, in half turns, and
+// reduced in binary64 (position / pi and its product with inv_freq are each rounded once, less than 2^-51 of the angle together), because in
+// binary32 an angle of 10^5 is off by 4e-3.  All heads of a token share its angles, and what norm weights and angles make of an
+// element's two factors: a warp takes one token, or, when there are few tokens, a part of its heads, whose angles it then turns again
+// (twice a token at 4900 tokens, five or six times at 600 to 2000).  It turns rot_dim / 2 angles into cosines and sines in its part of
+// shared memory and keeps the factors of its elements in registers for all of its heads.  Warps never wait for one another.
 //
 // A head belongs to kLanes lanes with kVecs 16-byte pieces each, neighbouring lanes next to each other.  Where the whole head turns in
 // pairs half a head apart, a lane holds both halves of its pairs.  Else the other half lies rot_dim / 16 pieces away: a shuffle when a

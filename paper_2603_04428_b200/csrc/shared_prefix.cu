@@ -832,8 +832,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_prefix_kernel(const __grid
     if (sm.abort_flag) {
       if (elect_one()) {                                 // the lane that issued the MMAs
         commit(&sm.drain);
-    #pragma unroll 1
-    for (uint32_t k = 0; k < kSpinLimit && !mbar_try_wait(&sm.drain, 0); ++k) {}
+#pragma unroll 1
+        for (uint32_t k = 0; k < kSpinLimit && !mbar_try_wait(&sm.drain, 0); ++k) {}
         raise_flag(P.flags, Q4KV_FLAG_INTERNAL);
       }
       __syncwarp();
@@ -999,7 +999,9 @@ TilePlan plan_tiles(const Layout& y, int n_agents, int n_groups, int max_kv_len,
 // of one agent.  alone: a fixed part, m for every agent and every 8 (d = 128) or 4 query heads to a KV head, and the merge by output rows.
 // list: m for every group and every 32 score rows (16 at d = 256; 16 or fewer at the other dimensions cost three quarters).  tiles: the
 // plan's units.  Fitted to 330 measured cases of 2 to 96 agents in 1 or 3 groups on 2000 to 32000 shared tokens with 200 of their own, 1
-// to 64 query heads to a KV head: the choice costs 0.6 % over the best of the three on average, 26 % at most.  Measured alone / list /
+// to 64 query heads to a KV head: the choice costs 0.6 % over the best of the three on average, 26 % at most.  It sees one average
+// group and the longest length only: one group beside agents that share nothing (32 on 32000 tokens and 32 others: all alone, where
+// the 32 on tiles would save 180 us by these estimates) and bounds far above the lengths are not its cases.  Measured alone / list /
 // tiles, one group unless said otherwise:
 //   8 KV heads of 4 query heads, d = 128, 4 agents on 8000     14.1 /  21.1 /  23.7      32 agents on 32000         206.4 / 99.4 / 43.7
 //   8 KV heads of 1, d = 128, 8 agents on 8000 tokens          21.2 /  20.8 /  23.8      on 32000                    58.0 / 32.1 / 40.2
